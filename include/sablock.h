@@ -280,6 +280,89 @@ sablock_status_t sablock_decode_attention(const sablock_params_t *p, int n_prob,
                                           const int *n_valid, float *out, float *lse,
                                           void *ws, size_t ws_bytes, sablock_stream_t stream);
 
+/* ---- Paged cache --------------------------------------------------------------------------------
+ * What a server decodes over once the prompts are compressed: rows of K and V of many sequences in pages of
+ * one pool, so that a sequence grows by a page at a time and none is padded to the longest.  Row r of
+ * sequence s lies in slot r % page_size of page table[s][r / page_size].  (The paper measures decoding over the
+ * compacted cache, Sec. 4.4; pages, rotation and the choice of pages are a service of this library.)
+ * Of the parameter block these calls read n_q_heads, n_kv_heads, head_dim and dtype; the strides are those of the
+ * description below.  All but the description's own fields is on the device, the lengths too: a call may be captured into
+ * a graph and replayed as the sequences grow.
+ *
+ * head_dim * element size must be a multiple of 16 bytes and head_dim at most 256; pools, strides, queries, tokens and
+ * workspace on 16-byte boundaries (SABLOCK_ERR_UNSUPPORTED otherwise; a misplaced workspace is SABLOCK_ERR_INVALID_ARG).  Any
+ * number of query heads per KV head, any page size.  Up to 4096 sequences of up to 2^30 rows.
+ * Device data that says what cannot be stays inside the buffers: lengths are taken as at least 0 and at most
+ * max_pages * page_size, and a page number outside [0, n_pages) is not followed (append drops the row, attention treats it as
+ * absent).  Two rows of one append that fall on the same place (a page that is in two tables) leave either's values. */
+typedef struct sablock_pages {
+    void *k, *v;                   /* dev pools [n_pages, page_size, Hkv, D] through the strides        */
+    void *bounds;                  /* dev [n_pages, Hkv, 2, D] (dtype of the block) or NULL: the smallest and the
+                                      largest value of every channel of the page's keys, kept by append  */
+    const int *table;              /* dev int32 [n_seqs, table_stride]: page numbers                    */
+    const int *seq_lens;           /* dev int32 [n_seqs]: rows of each sequence, rows being appended among them */
+    long long table_stride;        /* 0 = max_pages                                                     */
+    long long k_stride_page;       /* element strides of the pools; 0 = contiguous                      */
+    long long k_stride_row;
+    long long k_stride_head;
+    long long v_stride_page;
+    long long v_stride_row;
+    long long v_stride_head;
+    int n_seqs, n_pages, page_size, max_pages;   /* max_pages: entries of a table row that count        */
+    int reserved[4];
+} sablock_pages_t;
+
+size_t sablock_pages_sizeof(void);   /* sizeof(sablock_pages_t) as the library was built */
+
+/* Appends new tokens to their sequences, keys and queries rotated to their positions on the way.
+ *  cu_new dev int32[n_seqs+1] or NULL: sequence s has the tokens [cu_new[s], cu_new[s+1]) of the arrays below, which become its last rows
+ *  (the last of them row seq_lens[s] - 1); NULL: one token per sequence, n_tokens = n_seqs, and a sequence of length 0 (a padded
+ *  batch) takes none.  Tokens behind cu_new[n_seqs] and tokens that have no place are left alone, their q_out too.
+ *  k, v dev [n_tokens, Hkv, D], q dev [n_tokens, H, D] or NULL, heads contiguous, tokens k_stride, v_stride, q_stride elements apart (0 =
+ *  contiguous; so the parts of one projection's output can be passed in); q_out dev [n_tokens, H, D] contiguous, not
+ *  overlapping q; NULL with q.
+ *  inv_freq dev f32[rotary_dim / 2] or NULL (rotary_dim = 0: no rotation; how rows that the compression retained, which are
+ *  rotated already, go into pages): the first rotary_dim channels of a head are turned in pairs (i, i + rotary_dim / 2), or
+ *  (2 i, 2 i + 1) with interleaved, by the angle position * inv_freq[i].  positions dev int32[n_tokens] or NULL (the
+ *  row number).  After a compression a token's position is not its row: pass positions.
+ *  The angle is formed in double and the rotation computed in fp32, rounded once to dtype.
+ *  With bounds: those of the pages that rows fall into are brought up to date; the first row of a page starts them anew.  Bounds hold no number
+ *  where a key does not. */
+sablock_status_t sablock_paged_append(const sablock_params_t *p, const sablock_pages_t *pages, int n_tokens,
+                                      const int *cu_new, const void *k, long long k_stride,
+                                      const void *v, long long v_stride, const void *q, long long q_stride,
+                                      void *q_out, const int *positions, const float *inv_freq,
+                                      int rotary_dim, int interleaved, sablock_stream_t stream);
+
+/* The attention of one new query token per sequence over the rows of its pages (as sablock_decode_attention):
+ *  q dev [n_seqs, H, D] contiguous; out dev f32 [n_seqs, H, D]; lse dev f32 [n_seqs, H] or NULL.
+ *  selected NULL (n_selected 0): every row.  Otherwise dev int32 [n_seqs, Hkv, n_selected]: for each KV head the pages of the sequence
+ *  (0 for its first) whose rows count; of a sequence with fewer pages than n_selected as many entries are
+ *  read as it has pages; entries outside the sequence (-1) count nothing, an entry that stands twice counts twice.
+ *  A sequence without rows gets zeros and -inf.  Scratch from ws (sablock_paged_workspace_bytes, which depends on the heads, head_dim
+ *  and dtype only; 0 on invalid arguments); nothing in it has to be set.  Accumulation is fp32 in an order that the
+ *  lengths of the call fix. */
+size_t sablock_paged_workspace_bytes(const sablock_params_t *p, const sablock_pages_t *pages);
+sablock_status_t sablock_paged_attention(const sablock_params_t *p, const sablock_pages_t *pages, const void *q,
+                                         const int *selected, int n_selected, float *out, float *lse,
+                                         void *ws, size_t ws_bytes, sablock_stream_t stream);
+
+/* Which pages a token's queries should look at: for each KV head the n_selected pages whose bounds promise the largest logits,
+ *   score(page) = sum over the head's queries h and channels d of max(q[h][d] * lo[d], q[h][d] * hi[d]),
+ * in double, rounded once to fp32; ties go to the lower page.  The first n_first and the last n_last pages of a sequence are always
+ * in (n_first + n_last <= n_selected).  A score that is no number ranks above all others, a page that is not followed below.
+ *  selected dev int32 [n_seqs, Hkv, n_selected]: page indices, ascending; all pages and then -1 where there are not more.
+ * max_pages at most 49152. */
+sablock_status_t sablock_page_select(const sablock_params_t *p, const sablock_pages_t *pages, const void *q,
+                                     int n_selected, int n_first, int n_last, int *selected,
+                                     sablock_stream_t stream);
+
+/* Both: the attention over the pages that sablock_page_select chooses, which are left in selected. */
+sablock_status_t sablock_paged_sparse_attention(const sablock_params_t *p, const sablock_pages_t *pages, const void *q,
+                                                int n_selected, int n_first, int n_last, int *selected,
+                                                float *out, float *lse, void *ws, size_t ws_bytes,
+                                                sablock_stream_t stream);
+
 /* Per-stage timing (optional, for benchmarks).  While enabled, every fused call of this
  * thread records CUDA events on its stream between the stages, into the next of `slots`
  * event sets (round robin; the events are created on first use and kept until exit).

@@ -35,6 +35,8 @@ EXPORTS = [
     "sablock_params_sizeof", "sablock_workspace_region", "sablock_profile_enable", "sablock_profile_read",
     "sablock_profile_stage_name", "sablock_segment_static", "sablock_last_cuda_error", "sablock_read_status_detail",
     "sablock_decode_workspace_bytes", "sablock_decode_attention",
+    "sablock_pages_sizeof", "sablock_paged_append", "sablock_paged_workspace_bytes", "sablock_paged_attention",
+    "sablock_page_select", "sablock_paged_sparse_attention",
 ]
 
 
@@ -48,6 +50,17 @@ class Params(C.Structure):
         ("pool_kernel", C.c_int), ("pool_mode", C.c_int), ("budget_includes_window", C.c_int),
         ("delim_bitmap", C.c_void_p), ("vocab_size", C.c_int),
         ("score_impl", C.c_int), ("debug_sync", C.c_int), ("row_lse", C.c_void_p), ("reproducible", C.c_int), ("reserved", C.c_int * 5),
+    ]
+
+
+class Pages(C.Structure):
+    """Description of a paged cache (sablock_pages_t); make_pages fills one from its tensors."""
+    _fields_ = [
+        ("k", C.c_void_p), ("v", C.c_void_p), ("bounds", C.c_void_p), ("table", C.c_void_p), ("seq_lens", C.c_void_p),
+        ("table_stride", C.c_longlong),
+        ("k_stride_page", C.c_longlong), ("k_stride_row", C.c_longlong), ("k_stride_head", C.c_longlong),
+        ("v_stride_page", C.c_longlong), ("v_stride_row", C.c_longlong), ("v_stride_head", C.c_longlong),
+        ("n_seqs", C.c_int), ("n_pages", C.c_int), ("page_size", C.c_int), ("max_pages", C.c_int), ("reserved", C.c_int * 4),
     ]
 
 
@@ -73,6 +86,9 @@ def _load(path: str):
     l.sablock_params_sizeof.restype = C.c_size_t
     if l.sablock_params_sizeof() != C.sizeof(Params):
         raise ImportError("sablock_params_t layout mismatch between the library and the binding")
+    l.sablock_pages_sizeof.restype = C.c_size_t
+    if l.sablock_pages_sizeof() != C.sizeof(Pages):
+        raise ImportError("sablock_pages_t layout mismatch between the library and the binding")
     l.sablock_workspace_bytes.restype = C.c_size_t
     l.sablock_workspace_bytes.argtypes = [C.c_void_p, C.c_longlong, C.c_int, C.c_int, C.c_int]
     vp, ci, sz = C.c_void_p, C.c_int, C.c_size_t
@@ -91,10 +107,17 @@ def _load(path: str):
     l.sablock_compress_layers.argtypes = [vp, ci, ci, vp, vp, vp, vp, vp, ci, vp, ci, vp, vp, vp, vp, vp, sz, vp]
     l.sablock_compress_layers_host.argtypes = [vp, ci, ci, vp, vp, vp, vp, vp, ci, vp, ci, vp, vp, vp, vp,
                                                vp, vp, vp, vp, vp, vp, vp, vp, vp, sz, vp]
+    ll = C.c_longlong
+    l.sablock_paged_append.argtypes = [vp, vp, ci, vp, vp, ll, vp, ll, vp, ll, vp, vp, vp, ci, ci, vp]
+    l.sablock_paged_workspace_bytes.restype = sz
+    l.sablock_paged_workspace_bytes.argtypes = [vp, vp]
+    l.sablock_paged_attention.argtypes = [vp, vp, vp, vp, ci, vp, vp, vp, sz, vp]
+    l.sablock_page_select.argtypes = [vp, vp, vp, ci, ci, ci, vp, vp]
+    l.sablock_paged_sparse_attention.argtypes = [vp, vp, vp, ci, ci, ci, vp, vp, vp, vp, sz, vp]
     # The entry points that enqueue work, by their short names: through the C module where it is built.  A
     # sequence argument is a tuple or list there and a ctypes array here.
     for name in ("segment", "segment_static", "score", "select", "compact", "compress", "compress_layers", "compress_layers_host",
-                 "decode_attention"):
+                 "decode_attention", "paged_append", "paged_attention", "page_select", "paged_sparse_attention"):
         fn = getattr(l, "sablock_" + name)
         setattr(l, name, _fastcall.bind(C.cast(fn, C.c_void_p).value) if _fastcall else fn)
     l.decode_step = _fastcall.bind_decode(C.cast(l.sablock_decode_attention, C.c_void_p).value) if _fastcall else None
@@ -370,3 +393,136 @@ def decode_attention(p: Params, q: torch.Tensor, k_cache: torch.Tensor, v_cache:
     if code != OK:
         raise SablockError(code, "sablock_decode_attention")
     return (out, lse) if want_lse else out
+
+
+# ---- paged cache ------------------------------------------------------------------------------------------
+def _tensor(name: str, t: torch.Tensor, shape: Sequence[Optional[int]], dtype: torch.dtype, device) -> torch.Tensor:
+    """Refuses what the entry points cannot tell from an address."""
+    if t.dtype != dtype or t.device != device:
+        raise TypeError(f"{name}: {dtype} on {device} expected, got {t.dtype} on {t.device}")
+    if t.dim() != len(shape) or any(n is not None and n != m for n, m in zip(shape, t.shape)):
+        raise ValueError(f"{name}: shape {tuple(shape)} expected, got {tuple(t.shape)}")
+    return t
+
+
+def _contiguous(name: str, t: torch.Tensor) -> torch.Tensor:
+    if not t.is_contiguous():
+        raise ValueError(f"{name} must be contiguous")
+    return t
+
+
+def _token_stride(name: str, t: torch.Tensor) -> int:
+    """Elements from token to token of a [n, heads, D] tensor whose heads are contiguous."""
+    n, heads, d = t.shape
+    if n and ((d > 1 and t.stride(2) != 1) or (heads > 1 and t.stride(1) != d)):
+        raise ValueError(f"{name}: the heads of a token must be contiguous")
+    return t.stride(0) if n > 1 else 0
+
+
+def make_pages(p: Params, k_pages: torch.Tensor, v_pages: torch.Tensor, table: torch.Tensor, seq_lens: torch.Tensor,
+               bounds: Optional[torch.Tensor] = None) -> Pages:
+    """Description of a paged cache: pools [n_pages, page_size, Hkv, D] (any strides with contiguous channels), table int32
+    [n_seqs, max_pages], seq_lens int32 [n_seqs], bounds [n_pages, Hkv, 2, D] where pages are to be selected.  It refers to the
+    tensors: what they hold at the time of a call counts, and they live as long as it does."""
+    dt, dev, hkv, d = {F32: torch.float32, BF16: torch.bfloat16}[p.dtype], k_pages.device, p.n_kv_heads, p.head_dim
+    _tensor("k_pages", k_pages, (None, None, hkv, d), dt, dev)
+    _tensor("v_pages", v_pages, k_pages.shape, dt, dev)
+    _tensor("table", table, (None, None), torch.int32, dev)
+    _contiguous("seq_lens", _tensor("seq_lens", seq_lens, (table.shape[0],), torch.int32, dev))
+    if table.shape[1] > 1 and table.stride(1) != 1:
+        raise ValueError("table: the entries of a sequence must be contiguous")
+    g = Pages()
+    for name, t in (("k", k_pages), ("v", v_pages)):
+        if d > 1 and t.stride(3) != 1:
+            raise ValueError(f"{name}_pages: channels must be contiguous")
+        setattr(g, name, t.data_ptr())
+        for i, what in enumerate(("page", "row", "head")):
+            setattr(g, f"{name}_stride_{what}", t.stride(i) if t.shape[i] > 1 else 0)
+    if bounds is not None:
+        g.bounds = _contiguous("bounds", _tensor("bounds", bounds, (k_pages.shape[0], hkv, 2, d), dt, dev)).data_ptr()
+    g.table, g.seq_lens = table.data_ptr(), seq_lens.data_ptr()
+    g.table_stride = table.stride(0) if table.shape[0] > 1 else 0
+    g.n_pages, g.page_size = k_pages.shape[:2]
+    g.n_seqs, g.max_pages = table.shape
+    g._refs = k_pages, v_pages, table, seq_lens, bounds
+    g._device, g._dtype = dev, dt
+    g._ws_bytes = int(lib().sablock_paged_workspace_bytes(C.addressof(p), C.addressof(g)))
+    return g
+
+
+def paged_workspace_bytes(p: Params, pages: Pages) -> int:
+    n = int(lib().sablock_paged_workspace_bytes(C.addressof(p), C.addressof(pages)))
+    if n == 0:
+        raise SablockError(2, "sablock_paged_workspace_bytes")
+    return n
+
+
+def paged_append(p: Params, pages: Pages, k: torch.Tensor, v: torch.Tensor, q: Optional[torch.Tensor] = None,
+                 positions: Optional[torch.Tensor] = None, inv_freq: Optional[torch.Tensor] = None, interleaved: bool = False,
+                 cu_new: Optional[torch.Tensor] = None, q_out: Optional[torch.Tensor] = None) -> Optional[torch.Tensor]:
+    """New tokens k, v [n, Hkv, D] become the last rows of their sequences (cu_new int32 [n_seqs + 1]: whose they are; None: one
+    each), keys and queries q [n, H, D] rotated by positions * inv_freq on the way.  Returns the rotated queries."""
+    dt, dev, d = pages._dtype, pages._device, p.head_dim
+    n = k.shape[0]
+    _tensor("k", k, (n, p.n_kv_heads, d), dt, dev)
+    _tensor("v", v, (n, p.n_kv_heads, d), dt, dev)
+    qs = 0
+    if q is not None:
+        _tensor("q", q, (n, p.n_q_heads, d), dt, dev)
+        qs = _token_stride("q", q)
+        if q_out is None:
+            q_out = torch.empty((n, p.n_q_heads, d), dtype=dt, device=dev)
+        else:
+            _contiguous("q_out", _tensor("q_out", q_out, (n, p.n_q_heads, d), dt, dev))
+    elif q_out is not None:
+        raise ValueError("q_out without q")
+    if positions is not None:
+        _contiguous("positions", _tensor("positions", positions, (n,), torch.int32, dev))
+    if inv_freq is not None:
+        _contiguous("inv_freq", _tensor("inv_freq", inv_freq, (None,), torch.float32, dev))
+    if cu_new is not None:
+        _contiguous("cu_new", _tensor("cu_new", cu_new, (pages.n_seqs + 1,), torch.int32, dev))
+    _check(lib().paged_append(C.addressof(p), C.addressof(pages), n, _ptr(cu_new), _ptr(k), _token_stride("k", k), _ptr(v),
+                              _token_stride("v", v), _ptr(q), qs, _ptr(q_out), _ptr(positions), _ptr(inv_freq),
+                              0 if inv_freq is None else 2 * inv_freq.shape[0], int(interleaved), _stream()), "sablock_paged_append")
+    return q_out
+
+
+def _paged_query(p: Params, pages: Pages, q: torch.Tensor, ws: Optional[torch.Tensor], want_lse: bool):
+    _contiguous("q", _tensor("q", q, (pages.n_seqs, p.n_q_heads, p.head_dim), pages._dtype, pages._device))
+    if ws is None:
+        ws = torch.empty(max(pages._ws_bytes, 16), dtype=torch.uint8, device=q.device)
+    out = torch.empty(q.shape, dtype=torch.float32, device=q.device)
+    return ws, out, torch.empty(q.shape[:2], dtype=torch.float32, device=q.device) if want_lse else None
+
+
+def paged_attention(p: Params, pages: Pages, q: torch.Tensor, selected: Optional[torch.Tensor] = None,
+                    ws: Optional[torch.Tensor] = None, want_lse: bool = False):
+    """Attention of one new token per sequence, q [n_seqs, H, D], over the rows of its pages, or over the pages selected int32
+    [n_seqs, Hkv, n].  Returns out f32 [n_seqs, H, D] (and lse [n_seqs, H])."""
+    ws, out, lse = _paged_query(p, pages, q, ws, want_lse)
+    n = 0
+    if selected is not None:
+        n = _contiguous("selected", _tensor("selected", selected, (pages.n_seqs, p.n_kv_heads, None), torch.int32, q.device)).shape[2]
+    _check(lib().paged_attention(C.addressof(p), C.addressof(pages), _ptr(q), _ptr(selected), n, _ptr(out), _ptr(lse), _ptr(ws),
+                                 ws.numel(), _stream()), "sablock_paged_attention")
+    return (out, lse) if want_lse else out
+
+
+def page_select(p: Params, pages: Pages, q: torch.Tensor, n_selected: int, n_first: int = 1, n_last: int = 1) -> torch.Tensor:
+    """The pages whose bounds promise the largest logits, per KV head: int32 [n_seqs, Hkv, n_selected], ascending, then -1."""
+    _contiguous("q", _tensor("q", q, (pages.n_seqs, p.n_q_heads, p.head_dim), pages._dtype, pages._device))
+    selected = torch.empty((pages.n_seqs, p.n_kv_heads, max(n_selected, 0)), dtype=torch.int32, device=q.device)
+    _check(lib().page_select(C.addressof(p), C.addressof(pages), _ptr(q), n_selected, n_first, n_last, _ptr(selected), _stream()),
+           "sablock_page_select")
+    return selected
+
+
+def paged_sparse_attention(p: Params, pages: Pages, q: torch.Tensor, n_selected: int, n_first: int = 1, n_last: int = 1,
+                           ws: Optional[torch.Tensor] = None, want_lse: bool = False):
+    """page_select and paged_attention over what it selects.  Returns (out, selected), and lse behind them."""
+    ws, out, lse = _paged_query(p, pages, q, ws, want_lse)
+    selected = torch.empty((pages.n_seqs, p.n_kv_heads, max(n_selected, 0)), dtype=torch.int32, device=q.device)
+    _check(lib().paged_sparse_attention(C.addressof(p), C.addressof(pages), _ptr(q), n_selected, n_first, n_last, _ptr(selected),
+                                        _ptr(out), _ptr(lse), _ptr(ws), ws.numel(), _stream()), "sablock_paged_sparse_attention")
+    return (out, selected, lse) if want_lse else (out, selected)

@@ -12,7 +12,7 @@ LIB = os.path.join(HERE, "libsablock.so")
 FASTCALL = os.path.join(HERE, "_fastcall.so")
 SOURCES = ["sablock.cu"]
 HEADERS = ["common.cuh", "stages.cuh", "select.cuh", "score_simt.cuh", "score_tc.cuh", "score_fused.cuh", "score_flow.cuh", "score_pair.cuh", "score_x3.cuh",
-           "decode.cuh"]
+           "decode.cuh", "paged.cuh", "paged_attn.cuh"]
 
 
 def _stale(lib: str = LIB) -> bool:

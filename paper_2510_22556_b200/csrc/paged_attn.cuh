@@ -1,0 +1,702 @@
+// Attention of one new token per sequence over a paged cache: over all its rows, or over the pages chosen for each KV head
+// (page_select_kernel).  As in decode.cuh the work is a stream over K and V that the memory bounds, bf16 caches go through
+// warp-level matrix instructions with the fp32 weights in three bf16 pieces and fp32 caches through multiply-adds, and every sum
+// has a fixed order.  What differs:
+//
+// The lengths are on the device and ragged, so the host cannot cut the work.  A pair (sequence, KV head) has its rows in units; the
+// units of all pairs in order are one line, which the grid (as many CTAs as the device holds at once) cuts into equal shares.
+// A CTA adds the lengths up to find its share, which may start inside a pair, hold several pairs and end inside one.  Pairs that lie
+// in one share are written out; of the others every share leaves (accumulator, maximum, sum) in scratch, at most one at its
+// start and one at its end, and paged_merge_kernel, one block per share and head, adds up the pairs that begin in its share.
+//
+// A row is found through the table (and the list of chosen pages): the lanes of a warp look up the sixteen rows of a
+// chunk one turn before its copies go out (two turns before for the list), so the look-ups are never waited for.  Rows that do not
+// exist are not read: their 16-byte pieces are filled with zeros.
+#pragma once
+#include "decode.cuh"
+#include "paged.cuh"
+
+namespace sab {
+
+struct PagedAttnArgs {
+    Paged pg;
+    const void* q;                                   // [n_seqs][H][D]
+    const int* sel;                                  // [n_seqs][Hkv][n_sel], or NULL: all pages
+    int n_sel;
+    int H, Hkv, G, D;
+    int groups, group_heads;                         // head groups of a KV head, heads of a group (the last may have fewer)
+    bool same_place;                                 // K and V have the same strides
+    float c2;                                        // log2(e) / sqrt(D)
+    float* part;                                     // [2 x CTAs][group_heads][D + 2]: accumulator, max (log2 units), sum
+    int4* jobs;                                      // [CTAs]: first head row, heads, parts
+    float* out;                                      // [n_seqs][H][D]
+    float* lse;                                      // optional [n_seqs][H]
+    // rows of sequence s that the queries see through the list (a last page's absent rows count)
+    __device__ __forceinline__ int listed_rows(int s) const
+    {
+        const int rows = pg.rows_of(s);
+        return sel ? min(n_sel, pg.by_page.div(rows + pg.page_size - 1)) * pg.page_size : rows;
+    }
+};
+
+// A CTA's share [u, u_end) of the line of units; where it starts: sequence s, `skip` units into the units of that sequence's pairs.
+struct PgShare {
+    long long u, u_end, quota, skip;
+    int s;
+};
+
+template <int THREADS, int UNIT>
+__device__ __forceinline__ PgShare pg_share(const PagedAttnArgs& a, int pairs)
+{
+    __shared__ long long warp_sum_s[THREADS / 32];
+    __shared__ long long skip_s;
+    __shared__ int s_s;
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    const int n = a.pg.n_seqs, per = (n + THREADS - 1) / THREADS;
+    const int s0 = min(tid * per, n), s1 = min(s0 + per, n);
+    auto units = [&](int s) { return max(1, (a.listed_rows(s) + UNIT - 1) / UNIT); };
+    long long mine = 0;
+    for (int s = s0; s < s1; ++s) mine += units(s);
+    long long upto = mine;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+        const long long x = __shfl_up_sync(0xffffffffu, upto, o);
+        if (lane >= o) upto += x;
+    }
+    if (lane == 31) warp_sum_s[warp] = upto;
+    __syncthreads();
+    long long total = 0;
+#pragma unroll
+    for (int w = 0; w < THREADS / 32; ++w) {
+        if (w < warp) upto += warp_sum_s[w];
+        total += warp_sum_s[w];
+    }
+    total *= pairs;
+    PgShare r;
+    r.quota = (total + gridDim.x - 1) / gridDim.x;
+    r.u = min((long long)blockIdx.x * r.quota, total);
+    r.u_end = min(r.u + r.quota, total);
+    long long before = (upto - mine) * pairs;
+    if (r.u >= before && r.u < before + mine * pairs)
+        for (int s = s0; s < s1; ++s) {
+            const long long here = (long long)units(s) * pairs;
+            if (r.u < before + here) {
+                s_s = s;
+                skip_s = r.u - before;
+                break;
+            }
+            before += here;
+        }
+    __syncthreads();
+    r.s = s_s;                                       // (not set where the share is empty, and not used)
+    r.skip = skip_s;
+    return r;
+}
+
+// Walks the pairs of a share: the segment of the pair that is in it.
+struct PgSegment {
+    int s, hk, g0, heads;                            // sequence, KV head, first head of the group, heads
+    int rows, row0, row1;                            // rows of the pair, and the segment's
+    bool first, last;                                // the segment starts (ends) the pair
+    long long units;                                 // of the pair
+};
+template <int UNIT>
+__device__ __forceinline__ PgSegment pg_segment(const PagedAttnArgs& a, const PgShare& sh, int s, int pair, int w)
+{
+    PgSegment g;
+    g.s = s;
+    g.hk = pair / a.groups;
+    const int gi = pair - g.hk * a.groups;
+    g.g0 = gi * a.group_heads;
+    g.heads = min(a.group_heads, a.G - g.g0);
+    g.rows = a.listed_rows(s);
+    g.units = max(1, (g.rows + UNIT - 1) / UNIT);
+    const long long n = min(g.units - w, sh.u_end - sh.u);
+    g.first = w == 0;
+    g.last = w + n == g.units;
+    g.row0 = w * UNIT;
+    g.row1 = (int)min((long long)g.rows, (w + n) * UNIT);
+    return g;
+}
+
+// The share's partial result of a segment: at the start of the share (0) or at its end (1).
+__device__ __forceinline__ float* pg_part(const PagedAttnArgs& a, const PgSegment& g, int h)
+{
+    return a.part + (((size_t)2 * blockIdx.x + (g.first ? 1 : 0)) * a.group_heads + h) * (a.D + 2);
+}
+__device__ __forceinline__ size_t pg_head(const PagedAttnArgs& a, const PgSegment& g) { return (size_t)g.s * a.H + (size_t)g.hk * a.G + g.g0; }
+
+// Row look-ups of a warp's chunk, one row per lane: page list, then table, then offsets.
+struct PgRow {
+    int page, slot;                                  // page < 0: not there
+};
+struct PgLook {
+    const int *table, *sel;
+    int rows;                                        // of the segment, absolute end
+    int len;                                         // rows of the sequence
+};
+__device__ __forceinline__ PgLook pg_look(const PagedAttnArgs& a, const PgSegment& g)
+{
+    PgLook l;
+    l.table = a.pg.table + (long long)g.s * a.pg.table_stride;
+    l.sel = a.sel ? a.sel + ((size_t)g.s * a.Hkv + g.hk) * a.n_sel : nullptr;
+    l.rows = g.row1;
+    l.len = a.pg.rows_of(g.s);
+    return l;
+}
+// page of the sequence that row v of the list is in (-1: none), first half of a look-up
+__device__ __forceinline__ int pg_listed(const PagedAttnArgs& a, const PgLook& l, int v)
+{
+    if (v >= l.rows) return -1;
+    const int j = a.pg.by_page.div(v);
+    return l.sel ? l.sel[j] : j;
+}
+__device__ __forceinline__ PgRow pg_find(const PagedAttnArgs& a, const PgLook& l, int v, int j)
+{
+    PgRow r;
+    r.slot = v - a.pg.by_page.div(v) * a.pg.page_size;
+    const bool ok = (unsigned)j < (unsigned)a.pg.max_pages && (long long)j * a.pg.page_size + r.slot < l.len;
+    r.page = ok ? l.table[j] : -1;
+    return r;
+}
+
+// 16-byte asynchronous copy, or 16 bytes of zeros and nothing read
+__device__ __forceinline__ void cp_async16_or_zero(uint32_t dst, const void* src, bool there)
+{
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(there ? 16 : 0) : "memory");
+}
+
+// A pair's result, or the share's part of it, from the merged sums of a CTA.
+__device__ __forceinline__ void pg_emit(const PagedAttnArgs& a, const PgSegment& g, int h, int d, float sum, float m, float l)
+{
+    if (g.first && g.last) {
+        const size_t row = pg_head(a, g) + h;
+        a.out[row * a.D + d] = l == 0.f ? 0.f : sum / l;
+        if (a.lse && d == 0) a.lse[row] = l == 0.f ? -INFINITY : (m + log2f(l)) * 0.6931471805599453f;
+    } else {
+        float* dst = pg_part(a, g, h);
+        dst[d] = sum;
+        if (d == 0) { dst[a.D] = m; dst[a.D + 1] = l; }
+    }
+}
+
+// ---- bf16 -----------------------------------------------------------------------------------------------
+// As decode_mma_kernel (decode.cuh has the reasons): four warps, each with a private ring of 16-row chunks and its own online
+// softmax; a unit is 64 rows.  Up to four heads (Q4) go into rows 0-3 of the 16-row A operand and again into rows 4-7: rows 0-3
+// then carry the leading pieces of the weights, rows 8-11 the middle and rows 4-7 the last ones, one instruction for all three.
+// Otherwise heads come in NS sets of eight: the queries of the first set in rows 0-7, of the second in rows 8-15, one product for both;
+// the weights of a set take two instructions, half of the leading pieces in rows 0-7 of either (zeros there would make no numbers
+// of infinite values), the middle pieces in rows 8-15 of one and the last ones of the other.
+// head_dim is padded to DP with zeros that are not read from memory.
+constexpr int kPaThreads = 128;
+constexpr int kPaWarps = kPaThreads / 32;
+constexpr int kPaStages = 3;
+constexpr int kPaUnit = 16 * kPaWarps;
+__host__ __device__ constexpr int pa_smem(int DP) { return kPaWarps * kPaStages * 2 * 16 * DP * 2; }
+
+template <int NS, bool Q4, int DP>
+__global__ void __launch_bounds__(kPaThreads, DP == 256 ? 1 : 2)
+paged_mma_kernel(const __grid_constant__ PagedAttnArgs a)
+{
+    static_assert(!Q4 || NS == 1, "four heads are one set");
+    constexpr int PR = DP / 8;                       // 16-byte pieces of a row
+    constexpr int KS = DP / 16;                      // k-steps of the logits
+    constexpr int GP = Q4 ? 4 : 8 * NS;              // heads of a group
+    constexpr uint32_t kOp = 16 * DP * 2;            // bytes of a chunk of K or V
+    using bf16 = __nv_bfloat16;
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    extern __shared__ __align__(128) uint8_t pa_ring[];
+    __shared__ float ms[kPaWarps][GP], ls[kPaWarps][GP];
+    const uint32_t ring = smem_u32(pa_ring) + warp * kPaStages * 2 * kOp;
+    pdl_wait();
+    pdl_launch();
+    const int pairs = a.Hkv * a.groups;
+    PgShare sh = pg_share<kPaThreads, kPaUnit>(a, pairs);
+    if (tid == 0) a.jobs[blockIdx.x] = make_int4(0, 0, 0, 0);
+    if (sh.u >= sh.u_end) return;
+    int s = sh.s, pair, w;
+    {
+        const long long units = max(1, (a.listed_rows(s) + kPaUnit - 1) / kPaUnit);
+        pair = (int)(sh.skip / units);
+        w = (int)(sh.skip - pair * units);
+    }
+    const int n_pieces = a.D / 8;
+    while (sh.u < sh.u_end) {
+        const PgSegment g = pg_segment<kPaUnit>(a, sh, s, pair, w);
+        const PgLook look = pg_look(a, g);
+        const int chunks = g.row1 > g.row0 ? (g.row1 - g.row0 + 15) / 16 : 0;
+        const int n_it = (chunks - warp + kPaWarps - 1) / kPaWarps;
+        const bf16* kb = static_cast<const bf16*>(a.pg.k) + (size_t)g.hk * a.pg.k_head;
+        const bf16* vb = static_cast<const bf16*>(a.pg.v) + (size_t)g.hk * a.pg.v_head;
+        const int pc = lane % PR;
+        const bool piece_there = pc < n_pieces;
+
+        // this lane's row of the warp's chunk `it`
+        auto row_of = [&](int it) { return g.row0 + (it * kPaWarps + warp) * 16 + (lane & 15); };
+        auto listed = [&](int it) { return it < n_it ? pg_listed(a, look, row_of(it)) : -1; };
+        auto find = [&](int it, int j) { return it < n_it ? pg_find(a, look, row_of(it), j) : PgRow{-1, 0}; };
+        auto issue = [&](int it, const PgRow r) {
+            if (it < n_it) {
+                const uint32_t dst = ring + (uint32_t)(it % kPaStages) * 2 * kOp;
+                const bool ok = a.pg.holds(r.page);
+                const long long ko = ok ? (long long)r.page * a.pg.k_page + (long long)r.slot * a.pg.k_row : -1;
+                const long long vo = a.same_place ? ko : ok ? (long long)r.page * a.pg.v_page + (long long)r.slot * a.pg.v_row : -1;
+#pragma unroll
+                for (int i = 0; i < PR / 2; ++i) {
+                    const int rr = lane / PR + i * (32 / PR);
+                    const long long k_at = __shfl_sync(0xffffffffu, ko, rr);
+                    const long long v_at = a.same_place ? k_at : __shfl_sync(0xffffffffu, vo, rr);
+                    const bool there = k_at >= 0 && piece_there;
+                    const uint32_t o = dst + (uint32_t)(rr * PR + (pc ^ (rr & 7))) * 16;
+                    cp_async16_or_zero(o, kb + (there ? k_at + pc * 8 : 0), there);
+                    cp_async16_or_zero(o + kOp, vb + (there ? v_at + pc * 8 : 0), there);
+                }
+            }
+            cp_async_commit();
+        };
+        // copies of chunk it + kPaStages - 1 go out at chunk it; its rows have been looked up one turn, its pages two turns earlier
+        uint32_t there_ring[kPaStages - 1];          // which rows of the chunks in flight exist, a bit each
+        {
+            PgRow r[kPaStages - 1];
+            int j[kPaStages - 1];
+#pragma unroll
+            for (int t = 0; t < kPaStages - 1; ++t) j[t] = listed(t);
+#pragma unroll
+            for (int t = 0; t < kPaStages - 1; ++t) r[t] = find(t, j[t]);
+#pragma unroll
+            for (int t = 0; t < kPaStages - 1; ++t) {
+                there_ring[t] = __ballot_sync(0xffffffffu, a.pg.holds(r[t].page)) & 0xffffu;
+                issue(t, r[t]);
+            }
+        }
+        PgRow next = find(kPaStages - 1, listed(kPaStages - 1));
+        int next_j = listed(kPaStages);
+
+        uint32_t qa[KS][2 * NS];
+#pragma unroll
+        for (int n = 0; n < NS; ++n) {
+            const int hh = Q4 ? (lane >> 2) & 3 : 8 * n + (lane >> 2);
+            const bf16* qg = static_cast<const bf16*>(a.q) + (pg_head(a, g) + min(hh, g.heads - 1)) * a.D + 2 * (lane & 3);
+#pragma unroll
+            for (int ks = 0; ks < KS; ++ks)
+#pragma unroll
+                for (int x = 0; x < 2; ++x) {
+                    const int d = ks * 16 + x * 8;
+                    qa[ks][2 * n + x] = d < a.D ? *reinterpret_cast<const uint32_t*>(qg + d) : 0u;
+                }
+        }
+        float m[NS], l[NS], acc[NS][DP / 8][4];
+#pragma unroll
+        for (int n = 0; n < NS; ++n) {
+            m[n] = -INFINITY;
+            l[n] = 0.f;
+#pragma unroll
+            for (int i = 0; i < DP / 8; ++i)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) acc[n][i][e] = 0.f;
+        }
+        const int lr = lane & 7, mat = lane >> 3;
+        for (int it = 0; it < n_it; ++it) {
+            const uint32_t there = there_ring[0];
+#pragma unroll
+            for (int t = 0; t + 1 < kPaStages - 1; ++t) there_ring[t] = there_ring[t + 1];
+            there_ring[kPaStages - 2] = __ballot_sync(0xffffffffu, a.pg.holds(next.page)) & 0xffffu;
+            issue(it + kPaStages - 1, next);
+            next = find(it + kPaStages, next_j);
+            next_j = listed(it + kPaStages + 1);
+            cp_async_wait<kPaStages - 1>();
+            __syncwarp();
+            const uint32_t ks_base = ring + (uint32_t)(it % kPaStages) * 2 * kOp, vs_base = ks_base + kOp;
+            float c[2][4];
+#pragma unroll
+            for (int x = 0; x < 2; ++x)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) c[x][e] = 0.f;
+            {
+                const int row = lr + 8 * (mat >> 1);
+                const uint32_t base = ks_base + (uint32_t)row * PR * 16;
+#pragma unroll
+                for (int ks = 0; ks < KS; ++ks) {
+                    uint32_t b[4];
+                    ldsm_x4(base + (uint32_t)((2 * ks + (mat & 1)) ^ lr) * 16, b);
+                    const uint32_t a1 = NS == 2 ? qa[ks][2 * NS - 2] : 0u, a3 = NS == 2 ? qa[ks][2 * NS - 1] : 0u;
+                    mma_bf16(c[0], qa[ks][0], a1, qa[ks][1], a3, b[0], b[1]);
+                    mma_bf16(c[1], qa[ks][0], a1, qa[ks][1], a3, b[2], b[3]);
+                }
+            }
+            // logits of this thread's heads, rows row0, row0 + 1, row0 + 8, row0 + 9 of the chunk
+            const uint32_t seen = there >> (2 * (lane & 3));
+            uint32_t hi[NS][2], mid[NS][2], lo[NS][2];
+#pragma unroll
+            for (int n = 0; n < NS; ++n) {
+                float x[4];
+#pragma unroll
+                for (int t = 0; t < 2; ++t)
+#pragma unroll
+                    for (int e = 0; e < 2; ++e) x[2 * t + e] = (seen >> (8 * t + e)) & 1 ? c[t][2 * n + e] * a.c2 : -INFINITY;
+                const float mx = fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3]));
+                if (__any_sync(0xffffffffu, mx > m[n])) {
+                    float t = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 1));
+                    t = fmaxf(t, __shfl_xor_sync(0xffffffffu, t, 2));
+                    const float mn = fmaxf(m[n], t);
+                    const float sc = m[n] == -INFINITY ? 0.f : exp2f(m[n] - mn);
+                    m[n] = mn;
+                    l[n] *= sc;
+#pragma unroll
+                    for (int i = 0; i < DP / 8; ++i)
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) acc[n][i][e] *= sc;
+                }
+                const float mr = m[n] == -INFINITY ? 0.f : m[n];
+#pragma unroll
+                for (int t = 0; t < 2; ++t) {
+                    const float p0 = exp2f(x[2 * t] - mr), p1 = exp2f(x[2 * t + 1] - mr);
+                    l[n] += p0 + p1;
+                    constexpr float kShare = Q4 ? 1.f : 0.5f;      // of the leading piece in one instruction
+                    hi[n][t] = pack_bf16(kShare * p0, kShare * p1);
+                    const float q0 = fmaf(-1.f / kShare, __uint_as_float(hi[n][t] << 16), p0);
+                    const float q1 = fmaf(-1.f / kShare, __uint_as_float(hi[n][t] & 0xffff0000u), p1);
+                    mid[n][t] = pack_bf16(q0, q1);
+                    lo[n][t] = pack_bf16(q0 - __uint_as_float(mid[n][t] << 16), q1 - __uint_as_float(mid[n][t] & 0xffff0000u));
+                }
+                if constexpr (Q4) {
+#pragma unroll
+                    for (int t = 0; t < 2; ++t) {
+                        hi[n][t] = lane < 16 ? hi[n][t] : lo[n][t];
+                        mid[n][t] = lane < 16 ? mid[n][t] : 0u;
+                    }
+                }
+            }
+            {
+                const int row = lr + 8 * (mat & 1);
+                const uint32_t base = vs_base + (uint32_t)row * PR * 16;
+#pragma unroll
+                for (int i = 0; i < DP / 8; i += 2) {
+                    uint32_t b[4];
+                    ldsm_x4_trans(base + (uint32_t)((i + (mat >> 1)) ^ lr) * 16, b);
+#pragma unroll
+                    for (int n = 0; n < NS; ++n)
+#pragma unroll
+                        for (int t = 0; t < 2; ++t) {
+                            mma_bf16(acc[n][i + t], hi[n][0], mid[n][0], hi[n][1], mid[n][1], b[2 * t], b[2 * t + 1]);
+                            if constexpr (!Q4) mma_bf16(acc[n][i + t], hi[n][0], lo[n][0], hi[n][1], lo[n][1], b[2 * t], b[2 * t + 1]);
+                        }
+                }
+            }
+            __syncwarp();                            // the stage may be refilled
+        }
+        cp_async_wait<0>();
+        __syncthreads();
+        // ---- merge: the pieces, then the warps (over the ring), in a fixed order
+        float (*accs)[GP][DP] = reinterpret_cast<float (*)[GP][DP]>(pa_ring);
+        static_assert(kPaWarps * GP * DP * (int)sizeof(float) <= pa_smem(DP), "accumulators fit in the ring");
+#pragma unroll
+        for (int n = 0; n < NS; ++n) {
+            const int hh = Q4 ? (lane >> 2) & 3 : 8 * n + (lane >> 2);
+            const bool mine = !Q4 || lane < 16;
+            l[n] += __shfl_xor_sync(0xffffffffu, l[n], 1);
+            l[n] += __shfl_xor_sync(0xffffffffu, l[n], 2);
+#pragma unroll
+            for (int i = 0; i < DP / 8; ++i) {
+                float r[2];
+#pragma unroll
+                for (int e = 0; e < 2; ++e) {
+                    const float less = Q4 ? acc[n][i][2 + e] + __shfl_down_sync(0xffffffffu, acc[n][i][e], 16) : acc[n][i][2 + e];
+                    // an infinite value times a smaller piece is an infinity of either sign or, where the piece is zero, no
+                    // number: the leading piece alone says what the weight times the value is
+                    r[e] = isinf(acc[n][i][e]) ? acc[n][i][e] : acc[n][i][e] + less;
+                }
+                if (mine) *reinterpret_cast<float2*>(&accs[warp][hh][i * 8 + 2 * (lane & 3)]) = make_float2(r[0], r[1]);
+            }
+            if (mine && (lane & 3) == 0) { ms[warp][hh] = m[n]; ls[warp][hh] = l[n]; }
+        }
+        __syncthreads();
+        for (int i = tid; i < g.heads * a.D; i += kPaThreads) {
+            const int h = i / a.D, d = i - h * a.D;
+            float mx = -INFINITY;
+#pragma unroll
+            for (int v = 0; v < kPaWarps; ++v) mx = fmaxf(mx, ms[v][h]);
+            float sum = 0.f, lsum = 0.f;
+#pragma unroll
+            for (int v = 0; v < kPaWarps; ++v) {
+                if (ls[v][h] == 0.f) continue;       // (a warp without rows; one whose sum is no number counts)
+                const float wt = ms[v][h] == -INFINITY ? 1.f : exp2f(ms[v][h] - mx);
+                sum += accs[v][h][d] * wt;
+                lsum += ls[v][h] * wt;
+            }
+            pg_emit(a, g, h, d, sum, mx, lsum);
+        }
+        if (tid == 0 && g.first && !g.last) {
+            // the pair goes on in the next shares: the last unit of it is unit `end` of the line
+            const long long end = sh.u + g.units - 1;
+            a.jobs[blockIdx.x] = make_int4((int)pg_head(a, g), g.heads, (int)(end / sh.quota) - (int)blockIdx.x + 1, 0);
+        }
+        const long long n = min(g.units - w, sh.u_end - sh.u);
+        sh.u += n;
+        w = 0;
+        if (++pair == pairs) { pair = 0; ++s; }
+        __syncthreads();                             // the ring may be filled again
+    }
+}
+
+// ---- fp32 -----------------------------------------------------------------------------------------------
+// Multiply-adds.  A warp's chunk is eight rows: for the logits four lanes share a row (lane = 4 row + part, pieces part, part + 4, ...),
+// for the weighted values a lane owns columns and the weights go round through shared memory.
+constexpr int kPfRows = 8;
+constexpr int kPfStages = 3;
+constexpr int kPfUnit = kPfRows * kPaWarps;
+// Where piece p of row r of a chunk lies: the two rows that eight lanes read at a time for the logits fall into different banks.
+__device__ __forceinline__ int pf_piece(int r, int p) { return p ^ ((r & 1) << 2 | r >> 1); }
+__host__ __device__ constexpr int pf_smem(int DP) { return kPaWarps * kPfStages * 2 * kPfRows * DP * 4; }
+
+template <int GP, int DP>
+__global__ void __launch_bounds__(kPaThreads, DP == 256 ? 1 : 2)
+paged_fma_kernel(const __grid_constant__ PagedAttnArgs a)
+{
+    constexpr int PR = DP / 4;                       // 16-byte pieces of a row
+    constexpr uint32_t kOp = kPfRows * DP * 4;
+    constexpr int CW = DP / 32;                      // columns of a lane: 2, 4 or 8, in runs of at most four
+    constexpr int RUN = CW < 4 ? CW : 4;
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    extern __shared__ __align__(128) uint8_t pa_ring[];
+    __shared__ __align__(16) float qs[GP][DP];
+    __shared__ __align__(16) float ws[kPaWarps][kPfRows][GP];
+    __shared__ float ms[kPaWarps][GP], ls[kPaWarps][GP];
+    const uint32_t ring = smem_u32(pa_ring) + warp * kPfStages * 2 * kOp;
+    const uint8_t* ring_p = pa_ring + warp * kPfStages * 2 * kOp;
+    pdl_wait();
+    pdl_launch();
+    const int pairs = a.Hkv * a.groups;
+    PgShare sh = pg_share<kPaThreads, kPfUnit>(a, pairs);
+    if (tid == 0) a.jobs[blockIdx.x] = make_int4(0, 0, 0, 0);
+    if (sh.u >= sh.u_end) return;
+    int s = sh.s, pair, w;
+    {
+        const long long units = max(1, (a.listed_rows(s) + kPfUnit - 1) / kPfUnit);
+        pair = (int)(sh.skip / units);
+        w = (int)(sh.skip - pair * units);
+    }
+    const int n_pieces = a.D / 4;
+    while (sh.u < sh.u_end) {
+        const PgSegment g = pg_segment<kPfUnit>(a, sh, s, pair, w);
+        const PgLook look = pg_look(a, g);
+        const int chunks = g.row1 > g.row0 ? (g.row1 - g.row0 + kPfRows - 1) / kPfRows : 0;
+        const int n_it = (chunks - warp + kPaWarps - 1) / kPaWarps;
+        const float* kb = static_cast<const float*>(a.pg.k) + (size_t)g.hk * a.pg.k_head;
+        const float* vb = static_cast<const float*>(a.pg.v) + (size_t)g.hk * a.pg.v_head;
+        auto row_of = [&](int it) { return g.row0 + (it * kPaWarps + warp) * kPfRows + (lane & 7); };
+        auto listed = [&](int it) { return it < n_it ? pg_listed(a, look, row_of(it)) : -1; };
+        auto find = [&](int it, int j) { return it < n_it ? pg_find(a, look, row_of(it), j) : PgRow{-1, 0}; };
+        auto issue = [&](int it, const PgRow r) {
+            if (it < n_it) {
+                const uint32_t dst = ring + (uint32_t)(it % kPfStages) * 2 * kOp;
+                const bool ok = a.pg.holds(r.page);
+                const long long ko = ok ? (long long)r.page * a.pg.k_page + (long long)r.slot * a.pg.k_row : -1;
+                const long long vo = ok ? (long long)r.page * a.pg.v_page + (long long)r.slot * a.pg.v_row : -1;
+#pragma unroll
+                for (int i = 0; i < kPfRows * PR / 32; ++i) {
+                    const int id = i * 32 + lane, rr = id / PR, pc = id % PR;
+                    const long long k_at = __shfl_sync(0xffffffffu, ko, rr), v_at = __shfl_sync(0xffffffffu, vo, rr);
+                    const bool there = k_at >= 0 && pc < n_pieces;
+                    const uint32_t o = dst + (uint32_t)(rr * PR + pf_piece(rr, pc)) * 16;
+                    cp_async16_or_zero(o, kb + (there ? k_at + pc * 4 : 0), there);
+                    cp_async16_or_zero(o + kOp, vb + (there ? v_at + pc * 4 : 0), there);
+                }
+            }
+            cp_async_commit();
+        };
+        uint32_t there_ring[kPfStages - 1];
+        {
+            PgRow r[kPfStages - 1];
+            int j[kPfStages - 1];
+#pragma unroll
+            for (int t = 0; t < kPfStages - 1; ++t) j[t] = listed(t);
+#pragma unroll
+            for (int t = 0; t < kPfStages - 1; ++t) r[t] = find(t, j[t]);
+#pragma unroll
+            for (int t = 0; t < kPfStages - 1; ++t) {
+                there_ring[t] = __ballot_sync(0xffffffffu, a.pg.holds(r[t].page)) & 0xffu;
+                issue(t, r[t]);
+            }
+        }
+        PgRow next = find(kPfStages - 1, listed(kPfStages - 1));
+        int next_j = listed(kPfStages);
+        for (int i = tid; i < GP * DP; i += kPaThreads) {
+            const int h = i / DP, d = i - h * DP;
+            qs[h][d] = h < g.heads && d < a.D ? static_cast<const float*>(a.q)[(pg_head(a, g) + h) * a.D + d] * a.c2 : 0.f;
+        }
+        __syncthreads();
+        float m[GP], l[GP], acc[GP][CW];
+#pragma unroll
+        for (int h = 0; h < GP; ++h) {
+            m[h] = -INFINITY;
+            l[h] = 0.f;
+#pragma unroll
+            for (int e = 0; e < CW; ++e) acc[h][e] = 0.f;
+        }
+        const int row = lane >> 2, part = lane & 3;
+        for (int it = 0; it < n_it; ++it) {
+            const uint32_t there = there_ring[0];
+#pragma unroll
+            for (int t = 0; t + 1 < kPfStages - 1; ++t) there_ring[t] = there_ring[t + 1];
+            there_ring[kPfStages - 2] = __ballot_sync(0xffffffffu, a.pg.holds(next.page)) & 0xffu;
+            issue(it + kPfStages - 1, next);
+            next = find(it + kPfStages, next_j);
+            next_j = listed(it + kPfStages + 1);
+            cp_async_wait<kPfStages - 1>();
+            __syncwarp();
+            const uint8_t* kc = ring_p + (it % kPfStages) * 2 * kOp;
+            const uint8_t* vc = kc + kOp;
+            float x[GP];
+#pragma unroll
+            for (int h = 0; h < GP; ++h) x[h] = 0.f;
+#pragma unroll 4
+            for (int i = 0; i < PR / 4; ++i) {
+                const int pc = 4 * i + part;
+                const float4 kv = *reinterpret_cast<const float4*>(kc + (row * PR + pf_piece(row, pc)) * 16);
+#pragma unroll
+                for (int h = 0; h < GP; ++h) {
+                    const float4 qv = *reinterpret_cast<const float4*>(&qs[h][pc * 4]);
+                    x[h] = fmaf(qv.x, kv.x, fmaf(qv.y, kv.y, fmaf(qv.z, kv.z, fmaf(qv.w, kv.w, x[h]))));
+                }
+            }
+#pragma unroll
+            for (int h = 0; h < GP; ++h) {
+                x[h] += __shfl_xor_sync(0xffffffffu, x[h], 1);
+                x[h] += __shfl_xor_sync(0xffffffffu, x[h], 2);
+                if (!((there >> row) & 1)) x[h] = -INFINITY;
+                if (__any_sync(0xffffffffu, x[h] > m[h])) {
+                    float t = x[h];
+#pragma unroll
+                    for (int o = 4; o < 32; o <<= 1) t = fmaxf(t, __shfl_xor_sync(0xffffffffu, t, o));
+                    const float mn = fmaxf(m[h], t);
+                    const float sc = m[h] == -INFINITY ? 0.f : exp2f(m[h] - mn);
+                    m[h] = mn;
+                    l[h] *= sc;
+#pragma unroll
+                    for (int e = 0; e < CW; ++e) acc[h][e] *= sc;
+                }
+                const float p = exp2f(x[h] - (m[h] == -INFINITY ? 0.f : m[h]));
+                l[h] += p;                           // (the four lanes of a row hold the same)
+                if (part == 0) ws[warp][row][h] = p;
+            }
+            __syncwarp();
+#pragma unroll
+            for (int r = 0; r < kPfRows; ++r) {
+                float v[CW];
+#pragma unroll
+                for (int c = 0; c < CW / RUN; ++c) {
+                    const int d = (c * 32 + lane) * RUN;         // first column of the run
+                    const float* src = reinterpret_cast<const float*>(vc + (r * PR + pf_piece(r, d / 4)) * 16) + (d & 3);
+                    if constexpr (RUN == 4) {
+                        const float4 t = *reinterpret_cast<const float4*>(src);
+                        v[4 * c] = t.x; v[4 * c + 1] = t.y; v[4 * c + 2] = t.z; v[4 * c + 3] = t.w;
+                    } else {
+                        const float2 t = *reinterpret_cast<const float2*>(src);
+                        v[0] = t.x; v[1] = t.y;
+                    }
+                }
+#pragma unroll
+                for (int h = 0; h < GP; ++h) {
+                    const float p = ws[warp][r][h];
+#pragma unroll
+                    for (int e = 0; e < CW; ++e) acc[h][e] = fmaf(p, v[e], acc[h][e]);
+                }
+            }
+            __syncwarp();                            // the stage may be refilled, the weights written again
+        }
+        cp_async_wait<0>();
+        __syncthreads();
+        float (*accs)[GP][DP] = reinterpret_cast<float (*)[GP][DP]>(pa_ring);
+        static_assert(kPaWarps * GP * DP * (int)sizeof(float) <= pf_smem(DP), "accumulators fit in the ring");
+#pragma unroll
+        for (int h = 0; h < GP; ++h) {
+#pragma unroll
+            for (int o = 4; o < 32; o <<= 1) l[h] += __shfl_xor_sync(0xffffffffu, l[h], o);
+#pragma unroll
+            for (int e = 0; e < CW; ++e) accs[warp][h][((e / RUN) * 32 + lane) * RUN + e % RUN] = acc[h][e];
+            if (lane == 0) { ms[warp][h] = m[h]; ls[warp][h] = l[h]; }
+        }
+        __syncthreads();
+        for (int i = tid; i < g.heads * a.D; i += kPaThreads) {
+            const int h = i / a.D, d = i - h * a.D;
+            float mx = -INFINITY;
+#pragma unroll
+            for (int v = 0; v < kPaWarps; ++v) mx = fmaxf(mx, ms[v][h]);
+            float sum = 0.f, lsum = 0.f;
+#pragma unroll
+            for (int v = 0; v < kPaWarps; ++v) {
+                if (ls[v][h] == 0.f) continue;
+                const float wt = ms[v][h] == -INFINITY ? 1.f : exp2f(ms[v][h] - mx);
+                sum += accs[v][h][d] * wt;
+                lsum += ls[v][h] * wt;
+            }
+            pg_emit(a, g, h, d, sum, mx, lsum);
+        }
+        if (tid == 0 && g.first && !g.last) {
+            const long long end = sh.u + g.units - 1;
+            a.jobs[blockIdx.x] = make_int4((int)pg_head(a, g), g.heads, (int)(end / sh.quota) - (int)blockIdx.x + 1, 0);
+        }
+        const long long n = min(g.units - w, sh.u_end - sh.u);
+        sh.u += n;
+        w = 0;
+        if (++pair == pairs) { pair = 0; ++s; }
+        __syncthreads();
+    }
+}
+
+// ---- merging --------------------------------------------------------------------------------------------
+// Block (share, head): the pair that begins in the share and goes on in others, its parts in their order.  The weights go through
+// shared memory, and slices of threads take every n-th part each, so that the loads of the D-wide sums are independent of one another.
+constexpr int kPmThreads = 256;
+constexpr int kPmMaxParts = 1024;                    // shares of a call
+
+__global__ void __launch_bounds__(kPmThreads)
+paged_merge_kernel(const __grid_constant__ PagedAttnArgs a)
+{
+    const int b = blockIdx.x, h = blockIdx.y, tid = threadIdx.x;
+    __shared__ float w_s[kPmMaxParts], l_s[kPmMaxParts];
+    __shared__ float red[kPmThreads / 32];
+    __shared__ float num_s[kPmThreads];
+    pdl_wait();
+    pdl_launch();
+    const int4 job = a.jobs[b];
+    if (h >= job.y) return;
+    const int n = job.z, D = a.D;
+    // part i: of share b + i, at its end for the first, at its start for the others
+    auto part = [&](int i) { return a.part + (((size_t)2 * (b + i) + (i == 0 ? 1 : 0)) * a.group_heads + h) * (D + 2); };
+    float mx = -INFINITY;
+    for (int i = tid; i < n; i += kPmThreads) mx = fmaxf(mx, part(i)[D]);
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, o));
+    if ((tid & 31) == 0) red[tid >> 5] = mx;
+    __syncthreads();
+    float M = -INFINITY;
+#pragma unroll
+    for (int i = 0; i < kPmThreads / 32; ++i) M = fmaxf(M, red[i]);
+    for (int i = tid; i < n; i += kPmThreads) {
+        const float m = part(i)[D], l = part(i)[D + 1];
+        const float w = l == 0.f ? 0.f : m == -INFINITY ? 1.f : exp2f(m - M);
+        w_s[i] = w;
+        l_s[i] = l == 0.f ? 0.f : l * w;
+    }
+    __syncthreads();
+    const int dpad = (D + 31) / 32 * 32, slices = kPmThreads / dpad, slice = tid / dpad, d = tid - slice * dpad;
+    float num = 0.f;
+    if (slice < slices && d < D) {
+#pragma unroll 4
+        for (int i = slice; i < n; i += slices) num += w_s[i] == 0.f ? 0.f : part(i)[d] * w_s[i];
+        num_s[tid] = num;
+    }
+    __syncthreads();
+    if (slice == 0 && d < D) {
+        float den = 0.f, tot = 0.f;
+        for (int i = 0; i < n; ++i) den += l_s[i];
+        for (int i = 0; i < slices; ++i) tot += num_s[i * dpad + d];
+        const size_t row = (size_t)job.x + h;
+        a.out[row * D + d] = den == 0.f ? 0.f : tot / den;
+        if (a.lse && d == 0) a.lse[row] = den == 0.f ? -INFINITY : (M + log2f(den)) * 0.6931471805599453f;
+    }
+}
+
+}  // namespace sab

@@ -1,6 +1,6 @@
 // C ABI of the SABlock compression library (see include/sablock.h): argument validation,
 // workspace planning, TMA tensor maps and kernel launches.  Every step of the pass runs in the kernels of
-// stages.cuh, select.cuh and the score_*.cuh, decoding in those of decode.cuh; there is no host fallback.
+// stages.cuh, select.cuh and the score_*.cuh, decoding in those of decode.cuh and, over a paged cache, paged.cuh and paged_attn.cuh; there is no host fallback.
 #include <math.h>
 #include <stdio.h>
 #include <stdlib.h>
@@ -20,6 +20,8 @@
 #include "score_pair.cuh"
 #include "score_x3.cuh"
 #include "decode.cuh"
+#include "paged.cuh"
+#include "paged_attn.cuh"
 
 using namespace sab;
 
@@ -1075,6 +1077,141 @@ sablock_status_t launch_decode(const DecodeArgs& a, bool bf16, bool cluster, dim
     return SABLOCK_ERR_UNSUPPORTED;
 }
 
+// ---- paged cache ---------------------------------------------------------------------------
+bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15) == 0; }
+
+// The description of a paged cache, checked, as the kernels take it.  (Of the parameter block the heads, the head dimension and the type
+// count; the strides are the description's.)
+sablock_status_t paged_args(const sablock_params_t* p, const sablock_pages_t* pages, Paged* pg)
+{
+    if (!p || !pages) return SABLOCK_ERR_INVALID_ARG;
+    if (p->n_q_heads <= 0 || p->n_kv_heads <= 0 || p->n_q_heads % p->n_kv_heads || p->head_dim <= 0) return SABLOCK_ERR_INVALID_ARG;
+    if (p->dtype != SABLOCK_F32 && p->dtype != SABLOCK_BF16) return SABLOCK_ERR_INVALID_ARG;
+    if (!pages->k || !pages->v || !pages->table || !pages->seq_lens) return SABLOCK_ERR_INVALID_ARG;
+    if (pages->n_seqs < 1 || pages->n_pages < 1 || pages->page_size < 1 || pages->max_pages < 1) return SABLOCK_ERR_INVALID_ARG;
+    const long long stride[] = {pages->k_stride_page, pages->k_stride_row, pages->k_stride_head,
+                                pages->v_stride_page, pages->v_stride_row, pages->v_stride_head};
+    const int es = elem_size(p);
+    for (long long x : stride)
+        if (x < 0) return SABLOCK_ERR_INVALID_ARG;
+    if (pages->table_stride != 0 && pages->table_stride < pages->max_pages) return SABLOCK_ERR_INVALID_ARG;
+    if (p->n_q_heads > 4096 || p->head_dim > kPgMaxD || (p->head_dim * es) % 16 || pages->n_seqs > kPgMaxSeqs ||
+        (long long)pages->max_pages * pages->page_size > kPgMaxRows)
+        return SABLOCK_ERR_UNSUPPORTED;
+    for (long long x : stride)
+        if ((x * es) % 16) return SABLOCK_ERR_UNSUPPORTED;
+    if (!aligned16(pages->k) || !aligned16(pages->v) || !aligned16(pages->bounds)) return SABLOCK_ERR_UNSUPPORTED;
+    pg->k = pages->k; pg->v = pages->v; pg->bounds = pages->bounds;
+    pg->table = pages->table; pg->lens = pages->seq_lens;
+    pg->table_stride = pages->table_stride ? pages->table_stride : pages->max_pages;
+    pg->k_head = stride[2] ? stride[2] : p->head_dim;
+    pg->k_row = stride[1] ? stride[1] : (long long)p->n_kv_heads * p->head_dim;
+    pg->k_page = stride[0] ? stride[0] : pages->page_size * pg->k_row;
+    pg->v_head = stride[5] ? stride[5] : p->head_dim;
+    pg->v_row = stride[4] ? stride[4] : (long long)p->n_kv_heads * p->head_dim;
+    pg->v_page = stride[3] ? stride[3] : pages->page_size * pg->v_row;
+    pg->n_seqs = pages->n_seqs; pg->n_pages = pages->n_pages; pg->page_size = pages->page_size; pg->max_pages = pages->max_pages;
+    pg->max_rows = pages->max_pages * pages->page_size;
+    pg->by_page = fast_div((uint32_t)pages->page_size);
+    return SABLOCK_OK;
+}
+
+// The kernel of a call and its scratch.
+struct PagedPlan { int group_heads, groups, dp, ctas; size_t o_jobs, bytes; };
+PagedPlan paged_plan(const sablock_params_t* p)
+{
+    PagedPlan pl;
+    const int G = p->n_q_heads / p->n_kv_heads;
+    pl.dp = p->head_dim <= 64 ? 64 : p->head_dim <= 128 ? 128 : 256;
+    // Heads of a KV head that go through a CTA together; more are groups, which read the rows again
+    const int most = p->dtype == SABLOCK_BF16 && pl.dp <= 128 ? 16 : 8;
+    pl.group_heads = G <= 4 ? 4 : G <= 8 || most == 8 ? 8 : 16;
+    pl.groups = (G + pl.group_heads - 1) / pl.group_heads;
+    const int ctas = (pl.dp == 256 ? 1 : 2) * sm_count();
+    pl.ctas = ctas < kPmMaxParts ? ctas : kPmMaxParts;
+    pl.o_jobs = align_up(sizeof(float) * 2 * pl.ctas * pl.group_heads * (p->head_dim + 2));
+    pl.bytes = pl.o_jobs + align_up(sizeof(int4) * pl.ctas);
+    return pl;
+}
+
+template <int NS, bool Q4, int DP>
+sablock_status_t launch_paged_mma(const PagedAttnArgs& a, int ctas, cudaStream_t st)
+{
+    SAB_TRY(allow_smem<paged_mma_kernel<NS, Q4, DP>>(pa_smem(DP)));
+    return launch(paged_mma_kernel<NS, Q4, DP>, dim3(ctas), kPaThreads, pa_smem(DP), st, 1, a);
+}
+template <int GP, int DP>
+sablock_status_t launch_paged_fma(const PagedAttnArgs& a, int ctas, cudaStream_t st)
+{
+    SAB_TRY(allow_smem<paged_fma_kernel<GP, DP>>(pf_smem(DP)));
+    return launch(paged_fma_kernel<GP, DP>, dim3(ctas), kPaThreads, pf_smem(DP), st, 1, a);
+}
+
+sablock_status_t run_paged_attention(const sablock_params_t* p, const Paged& pg, const void* q, const int* sel, int n_sel, float* out,
+                                     float* lse, void* ws, size_t ws_bytes, cudaStream_t st)
+{
+    const PagedPlan pl = paged_plan(p);
+    if (!ws || ws_bytes < pl.bytes) return SABLOCK_ERR_WORKSPACE_TOO_SMALL;
+    if (!aligned16(ws)) return SABLOCK_ERR_INVALID_ARG;
+    PagedAttnArgs a;
+    a.pg = pg;
+    a.q = q; a.sel = sel; a.n_sel = n_sel;
+    a.H = p->n_q_heads; a.Hkv = p->n_kv_heads; a.G = a.H / a.Hkv; a.D = p->head_dim;
+    a.groups = pl.groups; a.group_heads = pl.group_heads;
+    a.same_place = pg.k_page == pg.v_page && pg.k_row == pg.v_row;
+    a.c2 = (float)(1.4426950408889634 / sqrt((double)p->head_dim));
+    a.part = static_cast<float*>(ws);
+    a.jobs = at<int4>(ws, pl.o_jobs);
+    a.out = out; a.lse = lse;
+    sablock_status_t rc = SABLOCK_ERR_UNSUPPORTED;
+#define SAB_PAGED(DP) \
+    if (pl.dp == DP) { \
+        if (p->dtype == SABLOCK_BF16) rc = pl.group_heads == 4 ? launch_paged_mma<1, true, DP>(a, pl.ctas, st) : pl.group_heads == 8 ? launch_paged_mma<1, false, DP>(a, pl.ctas, st) : launch_paged_mma<DP <= 128 ? 2 : 1, false, DP>(a, pl.ctas, st); \
+        else rc = pl.group_heads == 4 ? launch_paged_fma<4, DP>(a, pl.ctas, st) : launch_paged_fma<8, DP>(a, pl.ctas, st); \
+    }
+    SAB_PAGED(64)
+    SAB_PAGED(128)
+    SAB_PAGED(256)
+#undef SAB_PAGED
+    if (rc != SABLOCK_OK) return rc;
+    return launch(paged_merge_kernel, dim3(pl.ctas, pl.group_heads), kPmThreads, 0, st, 1, a);
+}
+
+// 16-byte pieces of a page's bounds per lane: 1, 2 or, in fp32, 4.
+template <typename T>
+sablock_status_t launch_page_select(const PageSelectArgs& a, int cluster, cudaStream_t st)
+{
+    const int smem = (int)align_up(sizeof(uint32_t) * a.pg.max_pages, 16);
+    const int per = (2 * a.D / PgVec<T>::kElems + 31) / 32;
+    const dim3 grid(cluster, a.pg.n_seqs * a.Hkv);
+#define SAB_SELECT(N) \
+    do { SAB_TRY(allow_smem<page_select_kernel<T, N>>(smem)); \
+         return launch(page_select_kernel<T, N>, grid, kPsThreads, smem, st, cluster, a, cluster); } while (0)
+    if (per <= 1) SAB_SELECT(1);
+    if constexpr (sizeof(T) == 4)
+        if (per > 2) SAB_SELECT(4);
+    SAB_SELECT(2);
+#undef SAB_SELECT
+}
+
+sablock_status_t run_page_select(const sablock_params_t* p, const Paged& pg, const void* q, int n_sel, int n_first, int n_last, int* sel,
+                                 cudaStream_t st)
+{
+    if (!pg.bounds || n_sel < 1 || n_first < 0 || n_last < 0 || n_first > n_sel || n_last > n_sel - n_first) return SABLOCK_ERR_INVALID_ARG;
+    if (pg.max_pages > kPsMaxPages) return SABLOCK_ERR_UNSUPPORTED;
+    const long long pairs = (long long)pg.n_seqs * p->n_kv_heads;
+    if (pairs > 65535 || (long long)n_sel * pg.page_size > kPgMaxRows) return SABLOCK_ERR_UNSUPPORTED;
+    PageSelectArgs a;
+    a.pg = pg;
+    a.q = q; a.sel = sel;
+    a.H = p->n_q_heads; a.Hkv = p->n_kv_heads; a.G = a.H / a.Hkv; a.D = p->head_dim;
+    a.n_sel = n_sel; a.n_first = n_first; a.n_last = n_last;
+    // CTAs that share a sequence's pages: while there are SMs for them and 64 pages (one turn of a CTA's warps) each
+    int c = 1;
+    while (c < kPsMaxCluster && pg.max_pages >= 128 * c && pairs * c * 2 <= 2 * sm_count()) c *= 2;
+    return p->dtype == SABLOCK_BF16 ? launch_page_select<__nv_bfloat16>(a, c, st) : launch_page_select<float>(a, c, st);
+}
+
 int rows_out(const sablock_params_t* p, int budget) { return p->budget_includes_window ? budget : budget + p->window; }
 
 }  // namespace
@@ -1224,6 +1361,13 @@ int sablock_test_host_chunk(const sablock_params_t* p, int n_layers, int n_seqs,
 }
 
 static int score_kernels(const Plan& pl) { return !pl.use_tc ? (pl.use_x3 ? 1 : 0) : pl.use_pair ? 3 : pl.use_flow ? 2 : 4; }
+
+// n / d as the paged kernels compute it, and the runs that an append has at most (host only).
+int sablock_test_fast_div(int n, int d) { return fast_div((uint32_t)d).div(n); }
+long long sablock_test_append_runs(long long n_tokens, int n_seqs, int run_rows, int one_each)
+{
+    return append_runs(n_tokens, n_seqs, run_rows, one_each != 0);
+}
 
 // Row splits of a decoding step, negative where they are a cluster (host only).
 int sablock_test_decode_splits(const sablock_params_t* p, int n_prob, int n_rows, size_t ws_bytes)
@@ -1454,6 +1598,98 @@ sablock_status_t sablock_decode_attention(const sablock_params_t* p, int n_prob,
     if (dp.cluster) return SABLOCK_OK;
     const int mt = kDecMergeSlices * ((p->head_dim + 31) / 32 * 32);
     return launch(decode_merge_kernel, dim3(p->n_q_heads, n_prob), mt, 0, st, 1, a);
+}
+
+// ---- paged cache -------------------------------------------------------------------------
+size_t sablock_pages_sizeof(void) { return sizeof(sablock_pages_t); }
+
+sablock_status_t sablock_paged_append(const sablock_params_t* p, const sablock_pages_t* pages, int n_tokens, const int* cu_new,
+                                      const void* k, long long k_stride, const void* v, long long v_stride, const void* q,
+                                      long long q_stride, void* q_out, const int* positions, const float* inv_freq, int rotary_dim,
+                                      int interleaved, sablock_stream_t stream)
+{
+    t_launches = 0;
+    AppendArgs a;
+    SAB_TRY(paged_args(p, pages, &a.pg));
+    if (!k || !v || !q != !q_out || n_tokens < 0 || k_stride < 0 || v_stride < 0 || q_stride < 0) return SABLOCK_ERR_INVALID_ARG;
+    if (!cu_new && n_tokens != pages->n_seqs) return SABLOCK_ERR_INVALID_ARG;
+    if (inv_freq ? rotary_dim < 2 || rotary_dim > p->head_dim || rotary_dim % 2 : rotary_dim != 0) return SABLOCK_ERR_INVALID_ARG;
+    const int es = elem_size(p);
+    a.H = p->n_q_heads; a.Hkv = p->n_kv_heads; a.G = a.H / a.Hkv; a.D = p->head_dim;
+    a.k_tok = k_stride ? k_stride : (long long)a.Hkv * a.D;
+    a.v_tok = v_stride ? v_stride : (long long)a.Hkv * a.D;
+    a.q_tok = q_stride ? q_stride : (long long)a.H * a.D;
+    if ((a.k_tok * es) % 16 || (a.v_tok * es) % 16 || (a.q_tok * es) % 16 || !aligned16(k) || !aligned16(v) || !aligned16(q) || !aligned16(q_out))
+        return SABLOCK_ERR_UNSUPPORTED;
+    if (n_tokens == 0) return SABLOCK_OK;
+    if (q) {   // a channel's partner is read by another thread than the one that writes it
+        const uintptr_t in = reinterpret_cast<uintptr_t>(q), out = reinterpret_cast<uintptr_t>(q_out);
+        const size_t row = (size_t)a.H * a.D * es, n = (size_t)n_tokens - 1;
+        if (in < out + n * row + row && out < in + n * (size_t)a.q_tok * es + row) return SABLOCK_ERR_INVALID_ARG;
+    }
+    a.q = q; a.k = k; a.v = v; a.q_out = q_out;
+    a.cu = cu_new; a.pos = positions; a.inv_freq = inv_freq;
+    a.half = rotary_dim / 2; a.interleaved = interleaved != 0; a.n_tokens = n_tokens;
+    // Runs of a page where its bounds are kept, of eight rows elsewhere; KV heads of a CTA: as many as there are threads for their pieces,
+    // fewer while that leaves SMs without two CTAs
+    const bool bounds = pages->bounds != nullptr;
+    a.run_rows = bounds ? pages->page_size : 8;
+    a.by_run = fast_div((uint32_t)a.run_rows);
+    const long long runs = append_runs(n_tokens, pages->n_seqs, a.run_rows, !cu_new);
+    const int pieces = a.D * es / 16;
+    a.heads = kApThreads / pieces;
+    if (a.heads > a.Hkv) a.heads = a.Hkv;
+    while (a.heads > 1 && runs * ((a.Hkv + a.heads - 1) / a.heads) < 2LL * sm_count()) a.heads = (a.heads + 1) / 2;
+    const dim3 grid((unsigned)runs, (a.Hkv + a.heads - 1) / a.heads);
+    cudaStream_t st = static_cast<cudaStream_t>(stream);
+    if (p->dtype == SABLOCK_BF16)
+        return bounds ? launch(paged_append_kernel<__nv_bfloat16, true>, grid, kApThreads, 0, st, 1, a)
+                      : launch(paged_append_kernel<__nv_bfloat16, false>, grid, kApThreads, 0, st, 1, a);
+    return bounds ? launch(paged_append_kernel<float, true>, grid, kApThreads, 0, st, 1, a)
+                  : launch(paged_append_kernel<float, false>, grid, kApThreads, 0, st, 1, a);
+}
+
+size_t sablock_paged_workspace_bytes(const sablock_params_t* p, const sablock_pages_t* pages)
+{
+    Paged pg;
+    return paged_args(p, pages, &pg) == SABLOCK_OK ? paged_plan(p).bytes : 0;
+}
+
+sablock_status_t sablock_paged_attention(const sablock_params_t* p, const sablock_pages_t* pages, const void* q, const int* selected,
+                                         int n_selected, float* out, float* lse, void* ws, size_t ws_bytes, sablock_stream_t stream)
+{
+    t_launches = 0;
+    Paged pg;
+    SAB_TRY(paged_args(p, pages, &pg));
+    if (!q || !out || (selected ? n_selected < 1 : n_selected != 0)) return SABLOCK_ERR_INVALID_ARG;
+    if (!aligned16(q) || (long long)n_selected * pages->page_size > kPgMaxRows) return SABLOCK_ERR_UNSUPPORTED;
+    return run_paged_attention(p, pg, q, selected, n_selected, out, lse, ws, ws_bytes, static_cast<cudaStream_t>(stream));
+}
+
+sablock_status_t sablock_page_select(const sablock_params_t* p, const sablock_pages_t* pages, const void* q, int n_selected, int n_first,
+                                     int n_last, int* selected, sablock_stream_t stream)
+{
+    t_launches = 0;
+    Paged pg;
+    SAB_TRY(paged_args(p, pages, &pg));
+    if (!q || !selected) return SABLOCK_ERR_INVALID_ARG;
+    if (!aligned16(q)) return SABLOCK_ERR_UNSUPPORTED;
+    return run_page_select(p, pg, q, n_selected, n_first, n_last, selected, static_cast<cudaStream_t>(stream));
+}
+
+sablock_status_t sablock_paged_sparse_attention(const sablock_params_t* p, const sablock_pages_t* pages, const void* q, int n_selected,
+                                                int n_first, int n_last, int* selected, float* out, float* lse, void* ws,
+                                                size_t ws_bytes, sablock_stream_t stream)
+{
+    t_launches = 0;
+    Paged pg;
+    SAB_TRY(paged_args(p, pages, &pg));
+    if (!q || !selected || !out) return SABLOCK_ERR_INVALID_ARG;
+    if (!aligned16(q)) return SABLOCK_ERR_UNSUPPORTED;
+    if (!ws || ws_bytes < paged_plan(p).bytes) return SABLOCK_ERR_WORKSPACE_TOO_SMALL;
+    if (!aligned16(ws)) return SABLOCK_ERR_INVALID_ARG;
+    SAB_TRY(run_page_select(p, pg, q, n_selected, n_first, n_last, selected, static_cast<cudaStream_t>(stream)));
+    return run_paged_attention(p, pg, q, selected, n_selected, out, lse, ws, ws_bytes, static_cast<cudaStream_t>(stream));
 }
 
 sablock_status_t sablock_compress_layers_host(const sablock_params_t* p, int n_layers, int n_seqs, const void* h_q_win,
