@@ -396,27 +396,47 @@ def decode_attention(p: Params, q: torch.Tensor, k_cache: torch.Tensor, v_cache:
 
 
 # ---- paged cache ------------------------------------------------------------------------------------------
-def _tensor(name: str, t: torch.Tensor, shape: Sequence[Optional[int]], dtype: torch.dtype, device) -> torch.Tensor:
-    """Refuses what the entry points cannot tell from an address."""
+def _refuse(name: str, t, dtype: torch.dtype, device, shape: Sequence[Optional[int]], how: str) -> None:
+    """Says what is wrong with a tensor that an entry point could not tell from an address."""
+    if not isinstance(t, torch.Tensor):
+        raise TypeError(f"{name}: a tensor expected, got {type(t).__name__}")
     if t.dtype != dtype or t.device != device:
         raise TypeError(f"{name}: {dtype} on {device} expected, got {t.dtype} on {t.device}")
     if t.dim() != len(shape) or any(n is not None and n != m for n, m in zip(shape, t.shape)):
         raise ValueError(f"{name}: shape {tuple(shape)} expected, got {tuple(t.shape)}")
-    return t
+    raise ValueError(f"{name}: {how}")
 
 
-def _contiguous(name: str, t: torch.Tensor) -> torch.Tensor:
-    if not t.is_contiguous():
-        raise ValueError(f"{name} must be contiguous")
-    return t
+def _fits(t: torch.Tensor, dtype: torch.dtype, device, shape) -> bool:
+    return t.dtype == dtype and t.device == device and t.shape == shape and t.is_contiguous()
 
 
-def _token_stride(name: str, t: torch.Tensor) -> int:
-    """Elements from token to token of a [n, heads, D] tensor whose heads are contiguous."""
-    n, heads, d = t.shape
+def _token_stride(t: torch.Tensor, dtype: torch.dtype, device, n: int, heads: int, d: int) -> int:
+    """Elements from token to token of a [n, heads, d] tensor whose heads are contiguous, -1 where it is none."""
+    if t.dtype != dtype or t.device != device or t.shape != (n, heads, d):
+        return -1
     if n and ((d > 1 and t.stride(2) != 1) or (heads > 1 and t.stride(1) != d)):
-        raise ValueError(f"{name}: the heads of a token must be contiguous")
+        return -1
     return t.stride(0) if n > 1 else 0
+
+
+if hasattr(_fastcall, "token_stride"):     # (not in a module that was built before it; a build makes it anew)
+    _fits, _token_stride = _fastcall.fits, _fastcall.token_stride
+
+
+def _contiguous(name: str, t: torch.Tensor, dtype: torch.dtype, device, shape) -> int:
+    """Address of a contiguous tensor of that type, device and shape; refuses others."""
+    if not (isinstance(t, torch.Tensor) and _fits(t, dtype, device, shape)):
+        _refuse(name, t, dtype, device, shape, "must be contiguous")
+    return t.data_ptr()
+
+
+def _tokens(name: str, t: torch.Tensor, dtype: torch.dtype, device, n: int, heads: int, d: int) -> int:
+    """Token stride of a [n, heads, d] tensor whose heads are contiguous; refuses others."""
+    s = _token_stride(t, dtype, device, n, heads, d) if isinstance(t, torch.Tensor) else -1
+    if s < 0:
+        _refuse(name, t, dtype, device, (n, heads, d), "the heads of a token must be contiguous")
+    return s
 
 
 def make_pages(p: Params, k_pages: torch.Tensor, v_pages: torch.Tensor, table: torch.Tensor, seq_lens: torch.Tensor,
@@ -425,29 +445,37 @@ def make_pages(p: Params, k_pages: torch.Tensor, v_pages: torch.Tensor, table: t
     [n_seqs, max_pages], seq_lens int32 [n_seqs], bounds [n_pages, Hkv, 2, D] where pages are to be selected.  It refers to the
     tensors: what they hold at the time of a call counts, and they live as long as it does."""
     dt, dev, hkv, d = {F32: torch.float32, BF16: torch.bfloat16}[p.dtype], k_pages.device, p.n_kv_heads, p.head_dim
-    _tensor("k_pages", k_pages, (None, None, hkv, d), dt, dev)
-    _tensor("v_pages", v_pages, k_pages.shape, dt, dev)
-    _tensor("table", table, (None, None), torch.int32, dev)
-    _contiguous("seq_lens", _tensor("seq_lens", seq_lens, (table.shape[0],), torch.int32, dev))
-    if table.shape[1] > 1 and table.stride(1) != 1:
-        raise ValueError("table: the entries of a sequence must be contiguous")
+    for name, t, shape in (("k_pages", k_pages, (None, None, hkv, d)), ("v_pages", v_pages, (*k_pages.shape[:2], hkv, d))):
+        if t.dtype != dt or t.device != dev or t.dim() != 4 or t.shape[2:] != (hkv, d) or t.shape != k_pages.shape or (d > 1 and t.stride(3) != 1):
+            _refuse(name, t, dt, dev, shape, "channels must be contiguous")
+    if table.dtype != torch.int32 or table.device != dev or table.dim() != 2 or (table.shape[1] > 1 and table.stride(1) != 1):
+        _refuse("table", table, torch.int32, dev, (None, None), "the entries of a sequence must be contiguous")
     g = Pages()
     for name, t in (("k", k_pages), ("v", v_pages)):
-        if d > 1 and t.stride(3) != 1:
-            raise ValueError(f"{name}_pages: channels must be contiguous")
         setattr(g, name, t.data_ptr())
         for i, what in enumerate(("page", "row", "head")):
             setattr(g, f"{name}_stride_{what}", t.stride(i) if t.shape[i] > 1 else 0)
-    if bounds is not None:
-        g.bounds = _contiguous("bounds", _tensor("bounds", bounds, (k_pages.shape[0], hkv, 2, d), dt, dev)).data_ptr()
-    g.table, g.seq_lens = table.data_ptr(), seq_lens.data_ptr()
-    g.table_stride = table.stride(0) if table.shape[0] > 1 else 0
     g.n_pages, g.page_size = k_pages.shape[:2]
     g.n_seqs, g.max_pages = table.shape
+    g.table, g.table_stride = table.data_ptr(), table.stride(0) if g.n_seqs > 1 else 0
+    g.seq_lens = _contiguous("seq_lens", seq_lens, torch.int32, dev, (g.n_seqs,))
+    if bounds is not None:
+        g.bounds = _contiguous("bounds", bounds, dt, dev, (g.n_pages, hkv, 2, d))
     g._refs = k_pages, v_pages, table, seq_lens, bounds
-    g._device, g._dtype = dev, dt
-    g._ws_bytes = int(lib().sablock_paged_workspace_bytes(C.addressof(p), C.addressof(g)))
+    g._dtype, g._device, g._q_shape = dt, dev, (g.n_seqs, p.n_q_heads, d)
+    # what the calls' outputs and scratch look like: empty_like of a tensor costs half of an empty
+    g._lse_like = torch.empty(1, device=dev).expand(g.n_seqs, p.n_q_heads)
+    g._ws_like = torch.empty(1, dtype=torch.uint8, device=dev).expand(
+        max(16, int(lib().sablock_paged_workspace_bytes(C.addressof(p), C.addressof(g)))))
+    g._sel_like = {}
     return g
+
+
+def _selection(p: Params, pages: Pages, n: int) -> torch.Tensor:
+    like = pages._sel_like.get(n)
+    if like is None:
+        like = pages._sel_like[n] = torch.empty(1, dtype=torch.int32, device=pages._device).expand(pages.n_seqs, p.n_kv_heads, max(int(n), 0))
+    return torch.empty_like(like)
 
 
 def paged_workspace_bytes(p: Params, pages: Pages) -> int:
@@ -462,58 +490,56 @@ def paged_append(p: Params, pages: Pages, k: torch.Tensor, v: torch.Tensor, q: O
                  cu_new: Optional[torch.Tensor] = None, q_out: Optional[torch.Tensor] = None) -> Optional[torch.Tensor]:
     """New tokens k, v [n, Hkv, D] become the last rows of their sequences (cu_new int32 [n_seqs + 1]: whose they are; None: one
     each), keys and queries q [n, H, D] rotated by positions * inv_freq on the way.  Returns the rotated queries."""
-    dt, dev, d = pages._dtype, pages._device, p.head_dim
+    dt, dev, hkv, H, d = pages._dtype, pages._device, p.n_kv_heads, p.n_q_heads, p.head_dim
     n = k.shape[0]
-    _tensor("k", k, (n, p.n_kv_heads, d), dt, dev)
-    _tensor("v", v, (n, p.n_kv_heads, d), dt, dev)
-    qs = 0
+    ks, vs, qs, q_at, out_at = _tokens("k", k, dt, dev, n, hkv, d), _tokens("v", v, dt, dev, n, hkv, d), 0, None, None
     if q is not None:
-        _tensor("q", q, (n, p.n_q_heads, d), dt, dev)
-        qs = _token_stride("q", q)
+        qs, q_at = _tokens("q", q, dt, dev, n, H, d), q.data_ptr()
         if q_out is None:
-            q_out = torch.empty((n, p.n_q_heads, d), dtype=dt, device=dev)
+            q_out = torch.empty_like(q)            # (contiguous: tokens that do not lie side by side are not kept apart)
+            out_at = q_out.data_ptr()
         else:
-            _contiguous("q_out", _tensor("q_out", q_out, (n, p.n_q_heads, d), dt, dev))
+            out_at = _contiguous("q_out", q_out, dt, dev, (n, H, d))
     elif q_out is not None:
         raise ValueError("q_out without q")
-    if positions is not None:
-        _contiguous("positions", _tensor("positions", positions, (n,), torch.int32, dev))
+    pos_at = None if positions is None else _contiguous("positions", positions, torch.int32, dev, (n,))
+    freq_at, rotary = None, 0
     if inv_freq is not None:
-        _contiguous("inv_freq", _tensor("inv_freq", inv_freq, (None,), torch.float32, dev))
-    if cu_new is not None:
-        _contiguous("cu_new", _tensor("cu_new", cu_new, (pages.n_seqs + 1,), torch.int32, dev))
-    _check(lib().paged_append(C.addressof(p), C.addressof(pages), n, _ptr(cu_new), _ptr(k), _token_stride("k", k), _ptr(v),
-                              _token_stride("v", v), _ptr(q), qs, _ptr(q_out), _ptr(positions), _ptr(inv_freq),
-                              0 if inv_freq is None else 2 * inv_freq.shape[0], int(interleaved), _stream()), "sablock_paged_append")
+        rotary = 2 * inv_freq.shape[0]
+        freq_at = _contiguous("inv_freq", inv_freq, torch.float32, dev, (rotary // 2,))
+    cu_at = None if cu_new is None else _contiguous("cu_new", cu_new, torch.int32, dev, (pages.n_seqs + 1,))
+    code = lib().paged_append(C.addressof(p), C.addressof(pages), n, cu_at, k.data_ptr(), ks, v.data_ptr(), vs, q_at, qs, out_at, pos_at,
+                              freq_at, rotary, 1 if interleaved else 0, _stream())
+    if code != OK:
+        raise SablockError(code, "sablock_paged_append")
     return q_out
-
-
-def _paged_query(p: Params, pages: Pages, q: torch.Tensor, ws: Optional[torch.Tensor], want_lse: bool):
-    _contiguous("q", _tensor("q", q, (pages.n_seqs, p.n_q_heads, p.head_dim), pages._dtype, pages._device))
-    if ws is None:
-        ws = torch.empty(max(pages._ws_bytes, 16), dtype=torch.uint8, device=q.device)
-    out = torch.empty(q.shape, dtype=torch.float32, device=q.device)
-    return ws, out, torch.empty(q.shape[:2], dtype=torch.float32, device=q.device) if want_lse else None
 
 
 def paged_attention(p: Params, pages: Pages, q: torch.Tensor, selected: Optional[torch.Tensor] = None,
                     ws: Optional[torch.Tensor] = None, want_lse: bool = False):
     """Attention of one new token per sequence, q [n_seqs, H, D], over the rows of its pages, or over the pages selected int32
     [n_seqs, Hkv, n].  Returns out f32 [n_seqs, H, D] (and lse [n_seqs, H])."""
-    ws, out, lse = _paged_query(p, pages, q, ws, want_lse)
-    n = 0
+    q_at = _contiguous("q", q, pages._dtype, pages._device, pages._q_shape)
+    sel_at, n = None, 0
     if selected is not None:
-        n = _contiguous("selected", _tensor("selected", selected, (pages.n_seqs, p.n_kv_heads, None), torch.int32, q.device)).shape[2]
-    _check(lib().paged_attention(C.addressof(p), C.addressof(pages), _ptr(q), _ptr(selected), n, _ptr(out), _ptr(lse), _ptr(ws),
-                                 ws.numel(), _stream()), "sablock_paged_attention")
+        n = selected.shape[-1]
+        sel_at = _contiguous("selected", selected, torch.int32, pages._device, (pages.n_seqs, p.n_kv_heads, n))
+    out = torch.empty_like(q, dtype=torch.float32)
+    lse = torch.empty_like(pages._lse_like) if want_lse else None
+    if ws is None:
+        ws = torch.empty_like(pages._ws_like)
+    code = lib().paged_attention(C.addressof(p), C.addressof(pages), q_at, sel_at, n, out.data_ptr(), lse.data_ptr() if want_lse else None,
+                                 ws.data_ptr(), ws.numel(), _stream())
+    if code != OK:
+        raise SablockError(code, "sablock_paged_attention")
     return (out, lse) if want_lse else out
 
 
 def page_select(p: Params, pages: Pages, q: torch.Tensor, n_selected: int, n_first: int = 1, n_last: int = 1) -> torch.Tensor:
     """The pages whose bounds promise the largest logits, per KV head: int32 [n_seqs, Hkv, n_selected], ascending, then -1."""
-    _contiguous("q", _tensor("q", q, (pages.n_seqs, p.n_q_heads, p.head_dim), pages._dtype, pages._device))
-    selected = torch.empty((pages.n_seqs, p.n_kv_heads, max(n_selected, 0)), dtype=torch.int32, device=q.device)
-    _check(lib().page_select(C.addressof(p), C.addressof(pages), _ptr(q), n_selected, n_first, n_last, _ptr(selected), _stream()),
+    q_at = _contiguous("q", q, pages._dtype, pages._device, pages._q_shape)
+    selected = _selection(p, pages, n_selected)
+    _check(lib().page_select(C.addressof(p), C.addressof(pages), q_at, n_selected, n_first, n_last, _ptr(selected), _stream()),
            "sablock_page_select")
     return selected
 
@@ -521,8 +547,14 @@ def page_select(p: Params, pages: Pages, q: torch.Tensor, n_selected: int, n_fir
 def paged_sparse_attention(p: Params, pages: Pages, q: torch.Tensor, n_selected: int, n_first: int = 1, n_last: int = 1,
                            ws: Optional[torch.Tensor] = None, want_lse: bool = False):
     """page_select and paged_attention over what it selects.  Returns (out, selected), and lse behind them."""
-    ws, out, lse = _paged_query(p, pages, q, ws, want_lse)
-    selected = torch.empty((pages.n_seqs, p.n_kv_heads, max(n_selected, 0)), dtype=torch.int32, device=q.device)
-    _check(lib().paged_sparse_attention(C.addressof(p), C.addressof(pages), _ptr(q), n_selected, n_first, n_last, _ptr(selected),
-                                        _ptr(out), _ptr(lse), _ptr(ws), ws.numel(), _stream()), "sablock_paged_sparse_attention")
+    q_at = _contiguous("q", q, pages._dtype, pages._device, pages._q_shape)
+    out = torch.empty_like(q, dtype=torch.float32)
+    lse = torch.empty_like(pages._lse_like) if want_lse else None
+    if ws is None:
+        ws = torch.empty_like(pages._ws_like)
+    selected = _selection(p, pages, n_selected)
+    code = lib().paged_sparse_attention(C.addressof(p), C.addressof(pages), q_at, n_selected, n_first, n_last, selected.data_ptr(),
+                                        out.data_ptr(), lse.data_ptr() if want_lse else None, ws.data_ptr(), ws.numel(), _stream())
+    if code != OK:
+        raise SablockError(code, "sablock_paged_sparse_attention")
     return (out, selected, lse) if want_lse else (out, selected)

@@ -147,7 +147,81 @@ static PyObject* bind_decode(PyObject* module, PyObject* address)
     return PyCFunction_New(&invoke_decode_def, address);
 }
 
-static PyMethodDef methods[] = {{"bind_decode", bind_decode, METH_O, "bind_decode(address): sablock_decode_attention for tensors"},
+/* What the calls over a paged cache check of a tensor, a few attributes each, in a third of the time that the same takes in
+ * Python.  fits(tensor, dtype, device, shape): whether it is that and contiguous; token_stride(tensor, dtype, device, n, heads, channels):
+ * elements from token to token of a tensor [n, heads, channels] whose heads are contiguous (0 where n < 2), -1 where it is none. */
+static PyObject *s_dtype, *s_device, *s_contiguous, *s_stride;
+
+/* 1: attribute `name` of t equals v; 0: it does not; -1: an error. */
+static int attr_equals(PyObject* t, PyObject* name, PyObject* v)
+{
+    PyObject* x = PyObject_GetAttr(t, name);
+    if (!x) return -1;
+    const int rc = x == v ? 1 : PyObject_RichCompareBool(x, v, Py_EQ);
+    Py_DECREF(x);
+    return rc;
+}
+
+static PyObject* fits(PyObject* module, PyObject* const* args, Py_ssize_t n)
+{
+    (void)module;
+    if (n != 4) return PyErr_Format(PyExc_TypeError, "%zd arguments, not 4", n);
+    int rc = attr_equals(args[0], s_dtype, args[1]);
+    if (rc == 1) rc = attr_equals(args[0], s_device, args[2]);
+    if (rc == 1) rc = attr_equals(args[0], s_shape, args[3]);
+    if (rc == 1) {
+        PyObject* x = PyObject_CallMethodNoArgs(args[0], s_contiguous);
+        if (!x) return NULL;
+        rc = x == Py_True;
+        Py_DECREF(x);
+    }
+    return rc < 0 ? NULL : PyBool_FromLong(rc);
+}
+
+/* Integers of a tuple of three. */
+static int take_three(PyObject* t, long long (*x)[3])
+{
+    if (!PyTuple_Check(t) || PyTuple_GET_SIZE(t) != 3) return 0;
+    for (int i = 0; i < 3; ++i) {
+        (*x)[i] = PyLong_AsLongLong(PyTuple_GET_ITEM(t, i));
+        if ((*x)[i] == -1 && PyErr_Occurred()) return -1;
+    }
+    return 1;
+}
+
+static PyObject* token_stride(PyObject* module, PyObject* const* args, Py_ssize_t n)
+{
+    (void)module;
+    long long want[3], size[3], stride[3];
+    if (n != 6) return PyErr_Format(PyExc_TypeError, "%zd arguments, not 6", n);
+    for (int i = 0; i < 3; ++i) {
+        want[i] = PyLong_AsLongLong(args[3 + i]);
+        if (want[i] == -1 && PyErr_Occurred()) return NULL;
+    }
+    int rc = attr_equals(args[0], s_dtype, args[1]);
+    if (rc == 1) rc = attr_equals(args[0], s_device, args[2]);
+    if (rc == 1) {
+        PyObject* x = PyObject_GetAttr(args[0], s_shape);
+        if (!x) return NULL;
+        rc = take_three(x, &size);
+        Py_DECREF(x);
+    }
+    if (rc == 1) rc = size[0] == want[0] && size[1] == want[1] && size[2] == want[2];
+    if (rc == 1) {
+        PyObject* x = PyObject_CallMethodNoArgs(args[0], s_stride);
+        if (!x) return NULL;
+        rc = take_three(x, &stride);
+        Py_DECREF(x);
+    }
+    if (rc < 0) return NULL;
+    if (rc == 1 && size[0] > 0) rc = (size[2] < 2 || stride[2] == 1) && (size[1] < 2 || stride[1] == size[2]);
+    return PyLong_FromLongLong(rc != 1 ? -1 : size[0] > 1 ? stride[0] : 0);
+}
+
+static PyMethodDef methods[] = {{"fits", (PyCFunction)(void (*)(void))fits, METH_FASTCALL, "fits(tensor, dtype, device, shape)"},
+                                {"token_stride", (PyCFunction)(void (*)(void))token_stride, METH_FASTCALL,
+                                 "token_stride(tensor, dtype, device, n, heads, channels)"},
+                                {"bind_decode", bind_decode, METH_O, "bind_decode(address): sablock_decode_attention for tensors"},
                                 {"bind", bind, METH_O, "bind(address): a callable for the entry point at that address"}, {NULL, NULL, 0, NULL}};
 static struct PyModuleDef module = {PyModuleDef_HEAD_INIT, "_fastcall", NULL, -1, methods, NULL, NULL, NULL, NULL};
 PyMODINIT_FUNC PyInit__fastcall(void)
@@ -155,5 +229,9 @@ PyMODINIT_FUNC PyInit__fastcall(void)
     s_data_ptr = PyUnicode_InternFromString("data_ptr");
     s_shape = PyUnicode_InternFromString("shape");
     s_numel = PyUnicode_InternFromString("numel");
-    return s_data_ptr && s_shape && s_numel ? PyModule_Create(&module) : NULL;
+    s_dtype = PyUnicode_InternFromString("dtype");
+    s_device = PyUnicode_InternFromString("device");
+    s_contiguous = PyUnicode_InternFromString("is_contiguous");
+    s_stride = PyUnicode_InternFromString("stride");
+    return s_data_ptr && s_shape && s_numel && s_dtype && s_device && s_contiguous && s_stride ? PyModule_Create(&module) : NULL;
 }

@@ -60,7 +60,7 @@ template <> struct PgVec<float> {
     {
         return make_uint4(__float_as_uint(x[0]), __float_as_uint(x[1]), __float_as_uint(x[2]), __float_as_uint(x[3]));
     }
-    __device__ static float rounded(float x) { return x; }
+    __device__ static float round(float x) { return x; }
 };
 template <> struct PgVec<__nv_bfloat16> {
     static constexpr int kElems = 8;
@@ -83,7 +83,7 @@ template <> struct PgVec<__nv_bfloat16> {
         }
         return make_uint4(w[0], w[1], w[2], w[3]);
     }
-    __device__ static float rounded(float x) { return __bfloat162float(__float2bfloat16_rn(x)); }
+    __device__ static __nv_bfloat16 round(float x) { return __float2bfloat16_rn(x); }
 };
 
 // The smaller (larger) of two values; no number where one of them is none.
@@ -104,15 +104,20 @@ __device__ __forceinline__ float max_nan(float a, float b)
 // New token t of sequence s becomes row r = lens[s] - (cu[s + 1] - t) (lens counts the new rows too).  Key and query channels
 // come in pairs (d, d + rd / 2), or (2 i, 2 i + 1) interleaved, and a pair is turned by the angle position * inv_freq[i]:
 //   x' = x cos - y sin,  y' = y cos + x sin,
-// in fp32, rounded once to the cache's type.  The angle needs more than 32 bits (at position 10^6 an fp32 angle is off by 0.03): its turns,
-// position * inv_freq / 2 pi, are formed in double, and what is left of them after the whole turns is small enough for fp32.
+// in fp32, rounded once to the cache's type.  The angle needs more than 32 bits (at position 10^6 an fp32 angle is off by 0.03): as turns,
+// position * inv_freq / 2 pi, it is formed modulo one in 64-bit fixed point, which at the last position is off by 2^-33.
 //
-// A CTA has one run of rows of one sequence (those of one page where bounds are kept, at most run_rows elsewhere; rows of a run are
-// aligned, so that a page's bounds have one writer) and some of the KV heads with their query heads.  It makes the cosines and sines of
-// kApTok tokens at a time for all its heads; then a thread owns one 16-byte piece of one head and walks the tokens, so that the
-// bounds stay in its registers.  Bound by memory: every row is read and written once.
+// A CTA has one run of rows of one sequence, at most kApRun of them and aligned, and some of the KV heads with their query heads.  A warp takes a token at a time (where
+// a run has fewer tokens than the CTA warps, several share one): it makes the token's cosines and sines once for all heads, and
+// its lanes take neighbouring heads, two pieces of a head each that hold each other's partners, four such loads at a time, so that what a
+// warp reads and writes is whole stretches of memory (lanes that took different tokens instead were a fifth slower).  Nothing is
+// shared between warps.  Bound by memory: every row is read and written once.
+//
+// Bounds of a page have one writer, a CTA that has all its new rows: the one that writes them, where a page has no more rows than a run
+// or a sequence has one new token; a second launch elsewhere, which reads the keys again (in L2).
 constexpr int kApThreads = 256;
-constexpr int kApTok = 16;
+constexpr int kApRun = 16;
+constexpr int kApBoundsRun = 32;                            // rows of a page whose bounds the same CTA makes
 
 struct AppendArgs {
     Paged pg;
@@ -124,7 +129,7 @@ struct AppendArgs {
     const float* inv_freq;                           // [half]
     int half, interleaved, n_tokens;
     int H, Hkv, G, D, heads;                         // heads: KV heads of a CTA
-    int run_rows;
+    int run_rows, slots, lane_bits;                  // slots: pairs of pieces of a head, for 2^lane_bits lanes
     FastDiv by_run;
 };
 
@@ -136,67 +141,142 @@ inline long long append_runs(long long n_tokens, int n_seqs, int run_rows, bool 
     return by_rows < n_tokens ? by_rows : n_tokens;
 }
 
-template <typename T>
-__device__ __forceinline__ uint4 rotate_piece(const uint4& raw, const T* row, int d0, const AppendArgs& a, const float* cs, const float* sn)
-{
-    constexpr int E = PgVec<T>::kElems;
-    const int rd = 2 * a.half;
-    if (d0 >= rd) return raw;
-    float x[E], y[E];
-    PgVec<T>::unpack(raw, x);
-    if (a.interleaved) {
-#pragma unroll
-        for (int e = 0; e < E; e += 2) {
-            const int i = (d0 + e) >> 1;
-            const bool in = d0 + e < rd;
-            const float c = in ? cs[i] : 1.f, s = in ? sn[i] : 0.f;
-            y[e] = in ? x[e] * c - x[e + 1] * s : x[e];
-            y[e + 1] = in ? x[e + 1] * c + x[e] * s : x[e + 1];
+// Pieces of a row: 16 bytes, or fewer where the halves of the rotation are not whole pieces of 16.
+template <int BYTES> struct Piece;
+template <> struct Piece<16> { using type = uint4; };
+template <> struct Piece<8> { using type = uint2; };
+template <> struct Piece<4> { using type = uint32_t; };
+template <> struct Piece<2> { using type = uint16_t; };
+
+// How the pairs of a rotation lie in a slot: nothing is turned, channel e of a piece with channel e of the other, neighbours of a piece.
+enum { kTurnNone = 0, kTurnAcross = 1, kTurnInside = 2 };
+
+template <typename T, int PB> struct ApSlot {
+    static constexpr int E = PB / (int)sizeof(T);
+    using V = typename Piece<PB>::type;
+    int d0, d1, how;                                 // first channels of the pieces; d1 < 0: there is no second
+    float c[E], s[E];                                // cosines and sines of the pairs
+
+    __device__ __forceinline__ void init(int slot, const AppendArgs& a)
+    {
+        // (neighbouring slots have neighbouring pieces: whole sectors go out at a time)
+        const int pairs = a.interleaved ? 0 : a.half / E;          // slots that hold a pair of partners
+        if (slot < pairs) {
+            d0 = slot * E;
+            d1 = d0 + a.half;
+            how = kTurnAcross;
+        } else {
+            const int rest = a.slots - pairs;
+            d0 = 2 * pairs * E + (slot - pairs) * E;
+            d1 = d0 + rest * E < a.D ? d0 + rest * E : -1;
+            how = d0 < 2 * a.half ? kTurnInside : kTurnNone;
         }
-    } else if (a.half % E == 0) {
-        // (a piece lies in one half, and so does its partner)
-        const bool upper = d0 >= a.half;
-        const int i0 = upper ? d0 - a.half : d0;
-        float z[E];
-        PgVec<T>::unpack(*reinterpret_cast<const uint4*>(row + (upper ? i0 : d0 + a.half)), z);
+    }
+    // cosines and sines of the slot from those of the token
+    __device__ __forceinline__ void angles(const float* cs, const float* sn, const AppendArgs& a)
+    {
+        if (how == kTurnNone) return;
 #pragma unroll
         for (int e = 0; e < E; ++e) {
-            const float c = cs[i0 + e], s = sn[i0 + e];
-            y[e] = upper ? x[e] * c + z[e] * s : x[e] * c - z[e] * s;
+            // inside: pairs 0 .. E / 2 - 1 are the first piece's, the others the second's
+            const int f = how == kTurnAcross ? d0 + e : min(e < E / 2 ? (d0 >> 1) + e : d1 < 0 ? 0 : (d1 >> 1) + e - E / 2, a.half - 1);
+            c[e] = cs[f];
+            s[e] = sn[f];
         }
-    } else {
+    }
+    __device__ __forceinline__ void turn(V& u, V& w, const AppendArgs& a) const
+    {
+        float x[E], y[E];
+        if (how == kTurnAcross) {
+            unpack(u, x);
+            unpack(w, y);
 #pragma unroll
-        for (int e = 0; e < E; ++e) {
-            const int d = d0 + e;
-            y[e] = x[e];
-            if (d < rd) {
-                const bool upper = d >= a.half;
-                const int i = upper ? d - a.half : d;
-                const float z = ld_as_float(row + (upper ? i : d + a.half));
-                y[e] = upper ? x[e] * cs[i] + z * sn[i] : x[e] * cs[i] - z * sn[i];
+            for (int e = 0; e < E; ++e) {
+                const float t = x[e] * c[e] - y[e] * s[e];
+                y[e] = y[e] * c[e] + x[e] * s[e];
+                x[e] = t;
+            }
+            u = pack(x);
+            w = pack(y);
+        } else if (how == kTurnInside) {
+            if constexpr (E >= 2) {
+                unpack(u, x);
+                unpack(w, y);
+#pragma unroll
+                for (int e = 0; e < E; e += 2) {
+                    inside(x[e], x[e + 1], c[e / 2], s[e / 2], d0 + e < 2 * a.half);
+                    inside(y[e], y[e + 1], c[E / 2 + e / 2], s[E / 2 + e / 2], d1 + e < 2 * a.half);
+                }
+                u = pack(x);
+                w = pack(y);
             }
         }
     }
-    return PgVec<T>::pack(y);
+    __device__ static __forceinline__ void inside(float& x, float& y, float c, float s, bool in)
+    {
+        const float t = x * c - y * s, z = y * c + x * s;
+        x = in ? t : x;
+        y = in ? z : y;
+    }
+    __device__ static __forceinline__ void unpack(const V& v, float (&x)[E])
+    {
+        const T* p = reinterpret_cast<const T*>(&v);
+#pragma unroll
+        for (int e = 0; e < E; ++e) x[e] = ld_as_float(p + e);
+    }
+    __device__ static __forceinline__ V pack(const float (&x)[E])
+    {
+        V v;
+        T* p = reinterpret_cast<T*>(&v);
+#pragma unroll
+        for (int e = 0; e < E; ++e) p[e] = PgVec<T>::round(x[e]);
+        return v;
+    }
+};
+
+// Smallest and largest values of a piece, packed as the piece is; no number where one is none.
+template <typename T> struct ApBounds;
+template <> struct ApBounds<float> {
+    __device__ static uint32_t least(uint32_t a, uint32_t b) { return __float_as_uint(min_nan(__uint_as_float(a), __uint_as_float(b))); }
+    __device__ static uint32_t most(uint32_t a, uint32_t b) { return __float_as_uint(max_nan(__uint_as_float(a), __uint_as_float(b))); }
+    static constexpr uint32_t kInf = 0x7f800000u, kNegInf = 0xff800000u;
+};
+template <> struct ApBounds<__nv_bfloat16> {
+    __device__ static uint32_t least(uint32_t a, uint32_t b)
+    {
+        uint32_t r;
+        asm("min.NaN.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
+        return r;
+    }
+    __device__ static uint32_t most(uint32_t a, uint32_t b)
+    {
+        uint32_t r;
+        asm("max.NaN.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
+        return r;
+    }
+    static constexpr uint32_t kInf = 0x7f807f80u, kNegInf = 0xff80ff80u;
+};
+template <typename T>
+__device__ __forceinline__ void widen(uint4 (&b)[2], const uint4& lo, const uint4& hi)
+{
+    using A = ApBounds<T>;
+    b[0] = make_uint4(A::least(b[0].x, lo.x), A::least(b[0].y, lo.y), A::least(b[0].z, lo.z), A::least(b[0].w, lo.w));
+    b[1] = make_uint4(A::most(b[1].x, hi.x), A::most(b[1].y, hi.y), A::most(b[1].z, hi.z), A::most(b[1].w, hi.w));
 }
 
-template <typename T, bool BOUNDS>
-__global__ void __launch_bounds__(kApThreads)
-paged_append_kernel(const __grid_constant__ AppendArgs a)
+// The run of a CTA: rows [ra, rb) of sequence s (none: rb <= ra), which begins at row `first`; its last row is that of token t_end - 1 - (len - rb).
+struct ApRun {
+    int s, len, t_end, first, ra, rb;
+};
+__device__ __forceinline__ ApRun append_run(const AppendArgs& a)
 {
-    constexpr int E = PgVec<T>::kElems;
-    const Paged& pg = a.pg;
-    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     __shared__ int run_s, run_j;
     __shared__ int warp_runs[kApThreads / 32];
-    __shared__ long long k_at[kApTok], v_at[kApTok];               // where a token's row goes (elements), -1: nowhere
-    __shared__ __align__(16) float cs[kApTok][kPgMaxD / 2], sn[kApTok][kPgMaxD / 2];
-    __shared__ __align__(16) float red[BOUNDS ? 2 * kApThreads * E : 4];
-    pdl_wait();
-    pdl_launch();
-
+    const Paged& pg = a.pg;
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     // rows [r0, r1) of sequence s are new; its tokens end before t_end
-    auto span = [&](int s, int& r0, int& r1, int& t_end) {
+    int r0, r1, t_end;
+    auto span = [&](int s) {
         const int len = pg.lens[s];
         int n = 1;
         t_end = s + 1;
@@ -208,13 +288,14 @@ paged_append_kernel(const __grid_constant__ AppendArgs a)
         r1 = min(len, pg.max_rows);
         return len;
     };
-    int s = blockIdx.x, j = -1, r0, r1, t_end;
+    ApRun run = {(int)blockIdx.x, 0, 0, 0, 0, 0};
+    int j = -1;
     if (a.cu) {
-        // the sequence and run of this CTA: runs counted over the sequences, a thread taking neighbouring ones
+        // runs counted over the sequences, a thread taking neighbouring ones
         const int per = (pg.n_seqs + kApThreads - 1) / kApThreads;
         const int s0 = min(tid * per, pg.n_seqs), s1 = min(s0 + per, pg.n_seqs);
         auto runs_of = [&](int i) {
-            span(i, r0, r1, t_end);
+            span(i);
             return r1 > r0 ? a.by_run.div(r1 - 1) - a.by_run.div(r0) + 1 : 0;
         };
         int mine = 0;
@@ -228,7 +309,8 @@ paged_append_kernel(const __grid_constant__ AppendArgs a)
         if (tid == 0) run_s = -1;
         if (lane == 31) warp_runs[warp] = upto;
         __syncthreads();
-        for (int w = 0; w < warp; ++w) upto += warp_runs[w];
+#pragma unroll
+        for (int w = 0; w < kApThreads / 32; ++w) upto += w < warp ? warp_runs[w] : 0;
         int left = (int)blockIdx.x - (upto - mine);
         if (left >= 0 && left < mine)
             for (int i = s0; i < s1; ++i) {
@@ -241,109 +323,153 @@ paged_append_kernel(const __grid_constant__ AppendArgs a)
                 left -= n;
             }
         __syncthreads();
-        s = run_s;
+        run.s = run_s;
         j = run_j;
-        if (s < 0) return;
+        if (run.s < 0) return run;
     }
-    const int len = span(s, r0, r1, t_end);
-    if (r1 <= r0) return;
-    if (j < 0) j = a.by_run.div(r0);
-    const long long first = (long long)j * a.run_rows;
-    const int ra = max(r0, (int)first), rb = (int)min((long long)r1, first + a.run_rows);
+    run.len = span(run.s);
+    if (r1 <= r0) return run;
+    run.t_end = t_end;
+    run.first = (j < 0 ? a.by_run.div(r0) : j) * a.run_rows;
+    run.ra = max(r0, run.first);
+    run.rb = (int)min((long long)r1, (long long)run.first + a.run_rows);
+    return run;
+}
 
-    const int h0 = blockIdx.y * a.heads, nk = min(a.heads, a.Hkv - h0);
-    const int PR = a.D / E, cols = nk * PR;
-    const int lanes = kApThreads / cols;                           // threads that share a piece's tokens (the host keeps cols <= kApThreads)
-    const int col = tid % cols, tl = tid / cols;
-    const int hk = h0 + col / PR, d0 = (col % PR) * E;
-    const T* kg = static_cast<const T*>(a.k) + (size_t)hk * a.D;
-    const T* vg = static_cast<const T*>(a.v) + (size_t)hk * a.D;
-    T* kp = static_cast<T*>(pg.k) + (size_t)hk * pg.k_head + d0;
-    T* vp = static_cast<T*>(pg.v) + (size_t)hk * pg.v_head + d0;
-    float lo[E], hi[E];
+// The bounds of the page whose rows a run is, columns [c0, c0 + n_cols) of 16-byte pieces of its keys: of the rows just written and,
+// unless they begin the page, of those before them.
+template <typename T>
+__device__ __forceinline__ void append_bounds(const AppendArgs& a, const ApRun& run, int c0, int n_cols)
+{
+    constexpr int E = PgVec<T>::kElems;
+    __shared__ uint4 red[2 * kApThreads];
+    const Paged& pg = a.pg;
+    const int tid = threadIdx.x, page = pg.table[(long long)run.s * pg.table_stride + pg.by_page.div(run.ra)];
+    if (!pg.holds(page)) return;
+    const int PR = a.D / E, at = run.ra - run.first, n = run.rb - run.ra;
+    for (int c = c0; c < c0 + n_cols; c += kApThreads) {
+        // a column to a thread, its rows shared where there are fewer columns than threads
+        const int cols = min(kApThreads, c0 + n_cols - c), lanes = kApThreads / cols, tl = tid / cols, col = tid - tl * cols;
+        const int h = (c + col) / PR, d = (c + col) % PR * E;
+        const T* src = static_cast<const T*>(pg.k) + (long long)page * pg.k_page + (long long)at * pg.k_row + (long long)h * pg.k_head + d;
+        constexpr uint32_t inf = ApBounds<T>::kInf, neg = ApBounds<T>::kNegInf;
+        uint4 b[2] = {make_uint4(inf, inf, inf, inf), make_uint4(neg, neg, neg, neg)};
+        if (tl < lanes)
+            for (int i = tl; i < n; i += 8 * lanes) {
+                uint4 x[8];
 #pragma unroll
-    for (int e = 0; e < E; ++e) { lo[e] = INFINITY; hi[e] = -INFINITY; }
-
-    for (int base = ra; base < rb; base += kApTok) {
-        const int nb = min(kApTok, rb - base);
-        const int t0 = t_end - (len - base);                       // token of row `base`
-        if (base > ra) __syncthreads();
-        for (int i = tid; i < nb * a.half; i += kApThreads) {
-            const int r = i / a.half, f = i - r * a.half;
-            const int p = a.pos ? a.pos[t0 + r] : base + r;
-            const double turns = (double)p * ((double)a.inv_freq[f] * 0.15915494309189533577);      // 1 / (2 pi)
-            const float left = (float)(turns - rint(turns));
-            float sv, cv;
-            sincospif(2.f * left, &sv, &cv);
-            cs[r][f] = cv;
-            sn[r][f] = sv;
-        }
-        if (tid < nb) {
-            const int row = base + tid, pj = pg.by_page.div(row), slot = row - pj * pg.page_size;
-            const int page = pg.table[(long long)s * pg.table_stride + pj];
-            const bool ok = pg.holds(page);
-            k_at[tid] = ok ? (long long)page * pg.k_page + (long long)slot * pg.k_row : -1;
-            v_at[tid] = ok ? (long long)page * pg.v_page + (long long)slot * pg.v_row : -1;
+                for (int t = 0; t < 8; ++t) x[t] = *reinterpret_cast<const uint4*>(src + (long long)min(i + t * lanes, n - 1) * pg.k_row);
+#pragma unroll
+                for (int t = 0; t < 8; ++t) widen<T>(b, x[t], x[t]);
+            }
+        red[tid] = b[0];
+        red[kApThreads + tid] = b[1];
+        __syncthreads();
+        if (tl == 0) {
+            for (int l = 1; l < lanes; ++l) widen<T>(b, red[l * cols + col], red[kApThreads + l * cols + col]);
+            T* dst = static_cast<T*>(pg.bounds) + (((size_t)page * a.Hkv + h) * 2) * a.D + d;
+            uint4 *lo = reinterpret_cast<uint4*>(dst), *hi = reinterpret_cast<uint4*>(dst + a.D);
+            if (at > 0) widen<T>(b, *lo, *hi);
+            *lo = b[0];
+            *hi = b[1];
         }
         __syncthreads();
-        if (tl < lanes) {
-#pragma unroll 2
-            for (int i = tl; i < nb; i += lanes) {
-                if (k_at[i] < 0) continue;
-                const T* row = kg + (long long)(t0 + i) * a.k_tok;
-                uint4 x = *reinterpret_cast<const uint4*>(row + d0);
-                const uint4 y = *reinterpret_cast<const uint4*>(vg + (long long)(t0 + i) * a.v_tok + d0);
-                x = rotate_piece<T>(x, row, d0, a, cs[i], sn[i]);
-                *reinterpret_cast<uint4*>(kp + k_at[i]) = x;
-                *reinterpret_cast<uint4*>(vp + v_at[i]) = y;
-                if constexpr (BOUNDS) {
-                    float f[E];
-                    PgVec<T>::unpack(x, f);
+    }
+}
+
+template <typename T, int PB, bool BOUNDS>
+__global__ void __launch_bounds__(kApThreads, BOUNDS ? 2 : 3)
+paged_append_kernel(const __grid_constant__ AppendArgs a)
+{
+    using Slot = ApSlot<T, PB>;
+    using V = typename Slot::V;
+    const Paged& pg = a.pg;
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    __shared__ float trig[kApThreads / 32][2][kPgMaxD / 2];
+    pdl_wait();
+    pdl_launch();
+
+    const ApRun run = append_run(a);
+    if (run.rb <= run.ra) return;
+    const int ra = run.ra, rb = run.rb;
+    const int* table = pg.table + (long long)run.s * pg.table_stride;
+
+    const int h0 = blockIdx.y * a.heads, nk = min(a.heads, a.Hkv - h0), n_rows = (a.q ? 2 + a.G : 2) * nk;
+    // warps: `rows` of them on rows of their own, the others share these rows' heads
+    constexpr int kWarps = kApThreads / 32;
+    int rows = 1;
+    while (rows < kWarps && rows < rb - ra) rows *= 2;
+    const int beside = 32 >> a.lane_bits;                          // heads that a warp has side by side
+    const int from = (warp / rows) * beside, step = (kWarps / rows) * beside, mine = lane >> a.lane_bits;
+    float *cs = trig[warp][0], *sn = trig[warp][1];
+    for (int r = ra + (warp & (rows - 1)); r < rb; r += rows) {
+        const int pj = pg.by_page.div(r), at = r - pj * pg.page_size, t = run.t_end - (run.len - r);
+        const int page = table[pj], p = a.pos ? a.pos[t] : r;
+        if (!pg.holds(page)) continue;
+        const T* ks = static_cast<const T*>(a.k) + (long long)t * a.k_tok + (long long)h0 * a.D;
+        const T* vs = static_cast<const T*>(a.v) + (long long)t * a.v_tok + (long long)h0 * a.D;
+        const T* qs = static_cast<const T*>(a.q) + (long long)t * a.q_tok + (long long)h0 * a.G * a.D;
+        T* kd = static_cast<T*>(pg.k) + (long long)page * pg.k_page + (long long)at * pg.k_row + (long long)h0 * pg.k_head;
+        T* vd = static_cast<T*>(pg.v) + (long long)page * pg.v_page + (long long)at * pg.v_row + (long long)h0 * pg.v_head;
+        T* qd = static_cast<T*>(a.q_out) + ((long long)t * a.H + (long long)h0 * a.G) * a.D;
+        bool made = a.half == 0;                                   // the token's cosines and sines
+        for (int slot = lane & ((1 << a.lane_bits) - 1); slot < (a.slots + (1 << a.lane_bits) - 1 >> a.lane_bits) << a.lane_bits; slot += 1 << a.lane_bits) {
+            Slot sl;
+            sl.init(min(slot, a.slots - 1), a);
+            const bool two = sl.d1 >= 0, in = slot < a.slots;
+            const int d1 = two ? sl.d1 : sl.d0;
+            bool known = false;
+            for (int u = from; u < n_rows; u += 4 * step) {
+                V x[4], y[4];
 #pragma unroll
-                    for (int e = 0; e < E; ++e) { lo[e] = min_nan(lo[e], f[e]); hi[e] = max_nan(hi[e], f[e]); }
+                for (int i = 0; i < 4; ++i) {
+                    const int h = min(u + i * step + mine, n_rows - 1);         // (no branch between the loads)
+                    const T* src = h < nk ? ks + h * a.D : h < 2 * nk ? vs + (h - nk) * a.D : qs + (h - 2 * nk) * a.D;
+                    x[i] = *reinterpret_cast<const V*>(src + sl.d0);
+                    y[i] = *reinterpret_cast<const V*>(src + d1);
                 }
-            }
-        }
-        if (a.q) {
-            const int qcols = cols * a.G, hq = h0 * a.G;
-            for (int i = tid; i < nb * qcols; i += kApThreads) {
-                const int r = i / qcols, c = i - r * qcols;
-                if (k_at[r] < 0) continue;
-                const int h = hq + c / PR, d = (c % PR) * E;
-                const T* row = static_cast<const T*>(a.q) + (long long)(t0 + r) * a.q_tok + (size_t)h * a.D;
-                const uint4 x = *reinterpret_cast<const uint4*>(row + d);
-                *reinterpret_cast<uint4*>(static_cast<T*>(a.q_out) + ((size_t)(t0 + r) * a.H + h) * a.D + d) =
-                    rotate_piece<T>(x, row, d, a, cs[r], sn[r]);
+                if (!made) {                                       // (while the first loads are on their way)
+                    made = true;
+                    __syncwarp();
+                    for (int f = lane; f < a.half; f += 32) {
+                        const double per = (double)a.inv_freq[f] * 0.15915494309189533577;       // 1 / (2 pi): turns from position to position
+                        const long long turn = (long long)((per - rint(per)) * 18446744073709551616.0);
+                        const int left = (int)(((unsigned long long)turn * (unsigned long long)(long long)p) >> 32);   // turns modulo one, in 2^-32
+                        sincospif((float)left * 0x1p-31f, &sn[f], &cs[f]);
+                    }
+                    __syncwarp();
+                }
+                if (!known) sl.angles(cs, sn, a);
+                known = true;
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const int h = u + i * step + mine;
+                    if (!in || h >= n_rows) continue;
+                    T* dst = h < nk ? kd + h * pg.k_head : h < 2 * nk ? vd + (h - nk) * pg.v_head : qd + (h - 2 * nk) * a.D;
+                    if (h < nk || h >= 2 * nk) sl.turn(x[i], y[i], a);
+                    *reinterpret_cast<V*>(dst + sl.d0) = x[i];
+                    if (two) *reinterpret_cast<V*>(dst + d1) = y[i];
+                }
             }
         }
     }
     if constexpr (BOUNDS) {
-        // the threads that share a piece, then what the page's earlier rows left; rows of this run are all in page j
-        const int page = pg.table[(long long)s * pg.table_stride + j];
-        if (!pg.holds(page)) return;
-        if (tl < lanes)
-#pragma unroll
-            for (int e = 0; e < E; ++e) { red[e * kApThreads + tid] = lo[e]; red[(E + e) * kApThreads + tid] = hi[e]; }
-        __syncthreads();
-        if (tl == 0) {
-            for (int l = 1; l < lanes; ++l)
-#pragma unroll
-                for (int e = 0; e < E; ++e) {
-                    lo[e] = min_nan(lo[e], red[e * kApThreads + l * cols + col]);
-                    hi[e] = max_nan(hi[e], red[(E + e) * kApThreads + l * cols + col]);
-                }
-            T* b = static_cast<T*>(pg.bounds) + (((size_t)page * a.Hkv + hk) * 2) * a.D + d0;
-            if (ra > first) {
-                float f[E], g[E];
-                PgVec<T>::unpack(*reinterpret_cast<const uint4*>(b), f);
-                PgVec<T>::unpack(*reinterpret_cast<const uint4*>(b + a.D), g);
-#pragma unroll
-                for (int e = 0; e < E; ++e) { lo[e] = min_nan(lo[e], f[e]); hi[e] = max_nan(hi[e], g[e]); }
-            }
-            *reinterpret_cast<uint4*>(b) = PgVec<T>::pack(lo);
-            *reinterpret_cast<uint4*>(b + a.D) = PgVec<T>::pack(hi);
-        }
+        __syncthreads();                             // the rows are written
+        append_bounds<T>(a, run, h0 * (a.D / PgVec<T>::kElems), nk * (a.D / PgVec<T>::kElems));
     }
+}
+
+// The bounds of pages of more rows than a CTA of the kernel above writes.
+template <typename T>
+__global__ void __launch_bounds__(kApThreads)
+paged_bounds_kernel(const __grid_constant__ AppendArgs a)
+{
+    pdl_wait();
+    pdl_launch();
+    const ApRun run = append_run(a);
+    if (run.rb <= run.ra) return;
+    const int all = a.Hkv * (a.D / PgVec<T>::kElems), per = (all + gridDim.y - 1) / gridDim.y, c0 = blockIdx.y * per;
+    if (c0 < all) append_bounds<T>(a, run, c0, min(per, all - c0));
 }
 
 // ---- which pages a token's queries look at --------------------------------------------------------------
@@ -357,9 +483,9 @@ paged_append_kernel(const __grid_constant__ AppendArgs a)
 // bf16, read by the whole warp) and leave the order-preserving integer images of the scores in the shared memory of CTA 0, which
 // finds the n_sel-th largest by counting into 1024 bins over the range of the keys, then over the range of the bin that it is
 // in, until all of a bin is in or its keys are equal.
-constexpr int kPsThreads = 256;
+constexpr int kPsThreads = 512;
 constexpr int kPsWarps = kPsThreads / 32;
-constexpr int kPsBins = 1024;
+constexpr int kPsBinBits = 10, kPsBins = 1 << kPsBinBits;
 constexpr int kPsMaxPages = 49152;                                 // keys of a sequence in shared memory (192 KB)
 constexpr int kPsMaxCluster = 8;
 constexpr uint32_t kKeyForced = 0xffffffffu, kKeyNan = 0xfffffffeu;
@@ -421,6 +547,14 @@ page_select_kernel(const __grid_constant__ PageSelectArgs a, int n_cta)
         for (int i = rank * kPsThreads + tid; i < a.n_sel; i += n_cta * kPsThreads) sel[i] = i < P ? i : -1;
         return;
     }
+    if (n_cta > 1) asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
+    const int* table = pg.table + (long long)s * pg.table_stride;
+    const int step = n_cta * kPsWarps * 8;
+    int next = -1;
+    {
+        const int j = (rank * kPsWarps + warp) * 8 + (lane & 7);
+        if (j < P) next = table[j];
+    }
     // weights of this lane's pieces: the first D elements of a page's bounds are its smallest values
     double w[NP][E];
     const int pieces = 2 * a.D / E;
@@ -435,22 +569,15 @@ page_select_kernel(const __grid_constant__ PageSelectArgs a, int n_cta)
         if (pc >= pieces) continue;
         const bool upper = pc * E >= a.D;
         const int d = pc * E - (upper ? a.D : 0);
-        for (int h = 0; h < a.G; ++h)
+        for (int h = 0; h < a.G; ++h) {
+            float x[E];
+            PgVec<T>::unpack(__ldg(reinterpret_cast<const uint4*>(q + (size_t)h * a.D + d)), x);
 #pragma unroll
-            for (int e = 0; e < E; ++e) {
-                const float x = ld_as_float(q + (size_t)h * a.D + d + e);
-                w[n][e] += upper ? (x < 0.f ? 0.0 : (double)x) : (x > 0.f ? 0.0 : (double)x);
-            }
+            for (int e = 0; e < E; ++e) w[n][e] += upper ? (x[e] < 0.f ? 0.0 : (double)x[e]) : (x[e] > 0.f ? 0.0 : (double)x[e]);
+        }
     }
-    if (n_cta > 1) cluster_sync();                                 // CTA 0 has started: its memory may be written
     const T* bounds = static_cast<const T*>(pg.bounds);
-    const int* table = pg.table + (long long)s * pg.table_stride;
-    const int step = n_cta * kPsWarps * 8;
-    int next = -1;
-    {
-        const int j = (rank * kPsWarps + warp) * 8 + (lane & 7);
-        if (j < P) next = table[j];
-    }
+    bool started = n_cta == 1;                                     // CTA 0's memory may be written
     for (int b = (rank * kPsWarps + warp) * 8; b < P; b += step) {
         const int page = next;
         next = b + step + (lane & 7) < P ? table[b + step + (lane & 7)] : -1;
@@ -461,11 +588,10 @@ page_select_kernel(const __grid_constant__ PageSelectArgs a, int n_cta)
         for (int i = 0; i < 8; ++i) {
             const int id = __shfl_sync(0xffffffffu, page, i);
             there[i] = b + i < P && pg.holds(id);
+            // (no branch between the loads: a page that is not there reads page 0, and its score is not used)
+            const uint4* row = reinterpret_cast<const uint4*>(bounds + ((size_t)(there[i] ? id : 0) * a.Hkv + hk) * 2 * a.D);
 #pragma unroll
-            for (int n = 0; n < NP; ++n)
-                x[i][n] = there[i] && lane + 32 * n < pieces
-                              ? __ldg(reinterpret_cast<const uint4*>(bounds + ((size_t)id * a.Hkv + hk) * 2 * a.D) + lane + 32 * n)
-                              : make_uint4(0, 0, 0, 0);
+            for (int n = 0; n < NP; ++n) x[i][n] = __ldg(row + min(lane + 32 * n, pieces - 1));
         }
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
@@ -479,6 +605,10 @@ page_select_kernel(const __grid_constant__ PageSelectArgs a, int n_cta)
             }
         }
         const double sum = sum8(v, lane);
+        if (!started) {
+            asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
+            started = true;
+        }
         const int i = lane >> 2;
         bool ok = false;
 #pragma unroll
@@ -490,15 +620,17 @@ page_select_kernel(const __grid_constant__ PageSelectArgs a, int n_cta)
             else ps_keys[j] = key;
         }
     }
+    if (!started) asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
     if (n_cta > 1) cluster_sync();
     else __syncthreads();
     if (rank != 0) return;
 
-    // the range of the keys
+    // the range of the keys but for the pages that are in anyway
     uint32_t kmin = 0xffffffffu, kmax = 0;
     for (int i = tid; i < P; i += kPsThreads) {
-        kmin = min(kmin, ps_keys[i]);
-        kmax = max(kmax, ps_keys[i]);
+        const uint32_t k = ps_keys[i];
+        kmin = min(kmin, k);
+        if (k != kKeyForced) kmax = max(kmax, k);
     }
     kmin = __reduce_min_sync(0xffffffffu, kmin);
     kmax = __reduce_max_sync(0xffffffffu, kmax);
@@ -507,10 +639,11 @@ page_select_kernel(const __grid_constant__ PageSelectArgs a, int n_cta)
 #pragma unroll
     for (int i = 0; i < kPsWarps; ++i) { kmin = min(kmin, ends[0][i]); kmax = max(kmax, ends[1][i]); }
     // keys above the range: `above` < n_sel; keys above or in it: at least n_sel
-    int above = 0, ties = 0;
-    while (true) {
+    int above = a.n_first + a.n_last, ties = 0;
+    if (above == a.n_sel) kmin = kmax = kKeyNan;
+    else while (true) {
         const uint32_t width = kmax - kmin;
-        const int shift = max(0, 22 - __clz(width | 1u));          // width >> shift < kPsBins
+        const int shift = max(0, 32 - kPsBinBits - __clz(width | 1u));     // width >> shift < kPsBins
         for (int i = tid; i < kPsBins; i += kPsThreads) hist[i] = 0;
         __syncthreads();
         for (int i = tid; i < P; i += kPsThreads) {
@@ -531,7 +664,8 @@ page_select_kernel(const __grid_constant__ PageSelectArgs a, int n_cta)
         }
         if (lane == 31) tot[0][warp] = upto;
         __syncthreads();
-        for (int i = 0; i < warp; ++i) upto += tot[0][i];
+#pragma unroll
+        for (int i = 0; i < kPsWarps; ++i) upto += i < warp ? tot[0][i] : 0;
         int before = above + upto - sum;                           // keys above this thread's bins
         if (before < a.n_sel && before + sum >= a.n_sel)
 #pragma unroll
@@ -555,7 +689,7 @@ page_select_kernel(const __grid_constant__ PageSelectArgs a, int n_cta)
         // (every thread has read found and tot before the next pass writes them: two barriers lie between)
     }
     // keys above kmax are in, and the first `ties` from kmin to kmax
-    const int per = (P + kPsThreads - 1) / kPsThreads;
+    const int per = ((P + kPsThreads - 1) / kPsThreads) | 1;       // (odd: a warp's threads read from 32 banks)
     const int j0 = min(tid * per, P), j1 = min(j0 + per, P);
     int n_hi = 0, n_eq = 0;
     for (int i = j0; i < j1; ++i) {
@@ -572,7 +706,11 @@ page_select_kernel(const __grid_constant__ PageSelectArgs a, int n_cta)
     __syncthreads();
     if (lane == 31) { tot[0][warp] = s_hi; tot[1][warp] = s_eq; }
     __syncthreads();
-    for (int i = 0; i < warp; ++i) { s_hi += tot[0][i]; s_eq += tot[1][i]; }
+#pragma unroll
+    for (int i = 0; i < kPsWarps; ++i) {
+        s_hi += i < warp ? tot[0][i] : 0;
+        s_eq += i < warp ? tot[1][i] : 0;
+    }
     int eq = s_eq - n_eq, at = s_hi - n_hi + min(eq, ties);
     for (int i = j0; i < j1; ++i) {
         const uint32_t k = ps_keys[i];

@@ -27,7 +27,7 @@ struct PagedAttnArgs {
     int groups, group_heads;                         // head groups of a KV head, heads of a group (the last may have fewer)
     bool same_place;                                 // K and V have the same strides
     float c2;                                        // log2(e) / sqrt(D)
-    float* part;                                     // [2 x CTAs][group_heads][D + 2]: accumulator, max (log2 units), sum
+    float* part;                                     // [2 x CTAs][group_heads][D + 4]: accumulator, max (log2 units), sum
     int4* jobs;                                      // [CTAs]: first head row, heads, parts
     float* out;                                      // [n_seqs][H][D]
     float* lse;                                      // optional [n_seqs][H]
@@ -122,13 +122,14 @@ __device__ __forceinline__ PgSegment pg_segment(const PagedAttnArgs& a, const Pg
 // The share's partial result of a segment: at the start of the share (0) or at its end (1).
 __device__ __forceinline__ float* pg_part(const PagedAttnArgs& a, const PgSegment& g, int h)
 {
-    return a.part + (((size_t)2 * blockIdx.x + (g.first ? 1 : 0)) * a.group_heads + h) * (a.D + 2);
+    return a.part + (((size_t)2 * blockIdx.x + (g.first ? 1 : 0)) * a.group_heads + h) * (a.D + 4);
 }
 __device__ __forceinline__ size_t pg_head(const PagedAttnArgs& a, const PgSegment& g) { return (size_t)g.s * a.H + (size_t)g.hk * a.G + g.g0; }
 
 // Row look-ups of a warp's chunk, one row per lane: page list, then table, then offsets.
 struct PgRow {
-    int page, slot;                                  // page < 0: not there
+    int page, slot;
+    bool ok;                                         // the row exists (if the page does)
 };
 struct PgLook {
     const int *table, *sel;
@@ -144,19 +145,20 @@ __device__ __forceinline__ PgLook pg_look(const PagedAttnArgs& a, const PgSegmen
     l.len = a.pg.rows_of(g.s);
     return l;
 }
-// page of the sequence that row v of the list is in (-1: none), first half of a look-up
+// page of the sequence that row v of the list is in, first half of a look-up.  (Loads are unconditional, and what they say about rows that
+// do not exist is ignored when it is used: a branch here would wait for them.)
 __device__ __forceinline__ int pg_listed(const PagedAttnArgs& a, const PgLook& l, int v)
 {
-    if (v >= l.rows) return -1;
-    const int j = a.pg.by_page.div(v);
+    const int j = a.pg.by_page.div(max(0, min(v, l.rows - 1)));       // (a sequence without rows has a first entry all the same)
     return l.sel ? l.sel[j] : j;
 }
 __device__ __forceinline__ PgRow pg_find(const PagedAttnArgs& a, const PgLook& l, int v, int j)
 {
     PgRow r;
     r.slot = v - a.pg.by_page.div(v) * a.pg.page_size;
-    const bool ok = (unsigned)j < (unsigned)a.pg.max_pages && (long long)j * a.pg.page_size + r.slot < l.len;
-    r.page = ok ? l.table[j] : -1;
+    const bool in = (unsigned)j < (unsigned)a.pg.max_pages;
+    r.ok = in && v < l.rows && (long long)j * a.pg.page_size + r.slot < l.len;
+    r.page = l.table[in ? j : 0];
     return r;
 }
 
@@ -233,12 +235,12 @@ paged_mma_kernel(const __grid_constant__ PagedAttnArgs a)
 
         // this lane's row of the warp's chunk `it`
         auto row_of = [&](int it) { return g.row0 + (it * kPaWarps + warp) * 16 + (lane & 15); };
-        auto listed = [&](int it) { return it < n_it ? pg_listed(a, look, row_of(it)) : -1; };
-        auto find = [&](int it, int j) { return it < n_it ? pg_find(a, look, row_of(it), j) : PgRow{-1, 0}; };
+        auto listed = [&](int it) { return pg_listed(a, look, row_of(it)); };
+        auto find = [&](int it, int j) { return pg_find(a, look, row_of(it), j); };
         auto issue = [&](int it, const PgRow r) {
             if (it < n_it) {
                 const uint32_t dst = ring + (uint32_t)(it % kPaStages) * 2 * kOp;
-                const bool ok = a.pg.holds(r.page);
+                const bool ok = r.ok && a.pg.holds(r.page);
                 const long long ko = ok ? (long long)r.page * a.pg.k_page + (long long)r.slot * a.pg.k_row : -1;
                 const long long vo = a.same_place ? ko : ok ? (long long)r.page * a.pg.v_page + (long long)r.slot * a.pg.v_row : -1;
 #pragma unroll
@@ -265,7 +267,7 @@ paged_mma_kernel(const __grid_constant__ PagedAttnArgs a)
             for (int t = 0; t < kPaStages - 1; ++t) r[t] = find(t, j[t]);
 #pragma unroll
             for (int t = 0; t < kPaStages - 1; ++t) {
-                there_ring[t] = __ballot_sync(0xffffffffu, a.pg.holds(r[t].page)) & 0xffffu;
+                there_ring[t] = __ballot_sync(0xffffffffu, r[t].ok && a.pg.holds(r[t].page)) & 0xffffu;
                 issue(t, r[t]);
             }
         }
@@ -300,7 +302,7 @@ paged_mma_kernel(const __grid_constant__ PagedAttnArgs a)
             const uint32_t there = there_ring[0];
 #pragma unroll
             for (int t = 0; t + 1 < kPaStages - 1; ++t) there_ring[t] = there_ring[t + 1];
-            there_ring[kPaStages - 2] = __ballot_sync(0xffffffffu, a.pg.holds(next.page)) & 0xffffu;
+            there_ring[kPaStages - 2] = __ballot_sync(0xffffffffu, next.ok && a.pg.holds(next.page)) & 0xffffu;
             issue(it + kPaStages - 1, next);
             next = find(it + kPaStages, next_j);
             next_j = listed(it + kPaStages + 1);
@@ -333,8 +335,8 @@ paged_mma_kernel(const __grid_constant__ PagedAttnArgs a)
 #pragma unroll
                 for (int t = 0; t < 2; ++t)
 #pragma unroll
-                    for (int e = 0; e < 2; ++e) x[2 * t + e] = (seen >> (8 * t + e)) & 1 ? c[t][2 * n + e] * a.c2 : -INFINITY;
-                const float mx = fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3]));
+                    for (int e = 0; e < 2; ++e) x[2 * t + e] = (seen >> (8 * t + e)) & 1 ? c[t][2 * n + e] : -INFINITY;
+                const float mx = fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3])) * a.c2;
                 if (__any_sync(0xffffffffu, mx > m[n])) {
                     float t = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 1));
                     t = fmaxf(t, __shfl_xor_sync(0xffffffffu, t, 2));
@@ -350,7 +352,7 @@ paged_mma_kernel(const __grid_constant__ PagedAttnArgs a)
                 const float mr = m[n] == -INFINITY ? 0.f : m[n];
 #pragma unroll
                 for (int t = 0; t < 2; ++t) {
-                    const float p0 = exp2f(x[2 * t] - mr), p1 = exp2f(x[2 * t + 1] - mr);
+                    const float p0 = exp2f(fmaf(x[2 * t], a.c2, -mr)), p1 = exp2f(fmaf(x[2 * t + 1], a.c2, -mr));
                     l[n] += p0 + p1;
                     constexpr float kShare = Q4 ? 1.f : 0.5f;      // of the leading piece in one instruction
                     hi[n][t] = pack_bf16(kShare * p0, kShare * p1);
@@ -485,12 +487,12 @@ paged_fma_kernel(const __grid_constant__ PagedAttnArgs a)
         const float* kb = static_cast<const float*>(a.pg.k) + (size_t)g.hk * a.pg.k_head;
         const float* vb = static_cast<const float*>(a.pg.v) + (size_t)g.hk * a.pg.v_head;
         auto row_of = [&](int it) { return g.row0 + (it * kPaWarps + warp) * kPfRows + (lane & 7); };
-        auto listed = [&](int it) { return it < n_it ? pg_listed(a, look, row_of(it)) : -1; };
-        auto find = [&](int it, int j) { return it < n_it ? pg_find(a, look, row_of(it), j) : PgRow{-1, 0}; };
+        auto listed = [&](int it) { return pg_listed(a, look, row_of(it)); };
+        auto find = [&](int it, int j) { return pg_find(a, look, row_of(it), j); };
         auto issue = [&](int it, const PgRow r) {
             if (it < n_it) {
                 const uint32_t dst = ring + (uint32_t)(it % kPfStages) * 2 * kOp;
-                const bool ok = a.pg.holds(r.page);
+                const bool ok = r.ok && a.pg.holds(r.page);
                 const long long ko = ok ? (long long)r.page * a.pg.k_page + (long long)r.slot * a.pg.k_row : -1;
                 const long long vo = ok ? (long long)r.page * a.pg.v_page + (long long)r.slot * a.pg.v_row : -1;
 #pragma unroll
@@ -515,7 +517,7 @@ paged_fma_kernel(const __grid_constant__ PagedAttnArgs a)
             for (int t = 0; t < kPfStages - 1; ++t) r[t] = find(t, j[t]);
 #pragma unroll
             for (int t = 0; t < kPfStages - 1; ++t) {
-                there_ring[t] = __ballot_sync(0xffffffffu, a.pg.holds(r[t].page)) & 0xffu;
+                there_ring[t] = __ballot_sync(0xffffffffu, r[t].ok && a.pg.holds(r[t].page)) & 0xffu;
                 issue(t, r[t]);
             }
         }
@@ -539,7 +541,7 @@ paged_fma_kernel(const __grid_constant__ PagedAttnArgs a)
             const uint32_t there = there_ring[0];
 #pragma unroll
             for (int t = 0; t + 1 < kPfStages - 1; ++t) there_ring[t] = there_ring[t + 1];
-            there_ring[kPfStages - 2] = __ballot_sync(0xffffffffu, a.pg.holds(next.page)) & 0xffu;
+            there_ring[kPfStages - 2] = __ballot_sync(0xffffffffu, next.ok && a.pg.holds(next.page)) & 0xffu;
             issue(it + kPfStages - 1, next);
             next = find(it + kPfStages, next_j);
             next_j = listed(it + kPfStages + 1);
@@ -646,57 +648,91 @@ paged_fma_kernel(const __grid_constant__ PagedAttnArgs a)
 }
 
 // ---- merging --------------------------------------------------------------------------------------------
-// Block (share, head): the pair that begins in the share and goes on in others, its parts in their order.  The weights go through
-// shared memory, and slices of threads take every n-th part each, so that the loads of the D-wide sums are independent of one another.
+// Block (share, head): the pair that begins in the share and goes on in others, its parts in their order.  A thread has four columns and
+// every n-th part; it asks for its first parts before the weights are known, which are found meanwhile.
 constexpr int kPmThreads = 256;
 constexpr int kPmMaxParts = 1024;                    // shares of a call
+constexpr int kPmAhead = 5;
 
 __global__ void __launch_bounds__(kPmThreads)
 paged_merge_kernel(const __grid_constant__ PagedAttnArgs a)
 {
-    const int b = blockIdx.x, h = blockIdx.y, tid = threadIdx.x;
-    __shared__ float w_s[kPmMaxParts], l_s[kPmMaxParts];
-    __shared__ float red[kPmThreads / 32];
-    __shared__ float num_s[kPmThreads];
+    const int b = blockIdx.x, h = blockIdx.y, tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    __shared__ float w_s[kPmMaxParts];
+    __shared__ float red[kPmThreads / 32], red_l[kPmThreads / 32];
+    __shared__ float4 num_s[kPmThreads];
     pdl_wait();
     pdl_launch();
     const int4 job = a.jobs[b];
     if (h >= job.y) return;
-    const int n = job.z, D = a.D;
+    const int n = job.z, D = a.D, quads = D / 4, slices = kPmThreads / quads, slice = tid / quads, d = 4 * (tid - slice * quads);
     // part i: of share b + i, at its end for the first, at its start for the others
-    auto part = [&](int i) { return a.part + (((size_t)2 * (b + i) + (i == 0 ? 1 : 0)) * a.group_heads + h) * (D + 2); };
+    auto part = [&](int i) { return a.part + (((size_t)2 * (b + i) + (i == 0 ? 1 : 0)) * a.group_heads + h) * (D + 4); };
+    const bool mine = slice < slices;
+    float4 x[kPmAhead];
+#pragma unroll
+    for (int t = 0; t < kPmAhead; ++t) {
+        const int i = slice + t * slices;
+        x[t] = *reinterpret_cast<const float4*>(part(min(i, n - 1)) + (mine ? d : 0));      // (no branch between the loads)
+    }
+    float2 ml[(kPmMaxParts + kPmThreads - 1) / kPmThreads];
     float mx = -INFINITY;
-    for (int i = tid; i < n; i += kPmThreads) mx = fmaxf(mx, part(i)[D]);
+#pragma unroll
+    for (int t = 0; t < kPmMaxParts / kPmThreads; ++t) {
+        const int i = tid + t * kPmThreads;
+        ml[t] = make_float2(-INFINITY, 0.f);
+        if (i < n) ml[t] = *reinterpret_cast<const float2*>(part(i) + D);
+        mx = fmaxf(mx, ml[t].x);
+    }
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, o));
-    if ((tid & 31) == 0) red[tid >> 5] = mx;
+    if (lane == 0) red[warp] = mx;
     __syncthreads();
-    float M = -INFINITY;
+    float M = -INFINITY, l = 0.f;
 #pragma unroll
     for (int i = 0; i < kPmThreads / 32; ++i) M = fmaxf(M, red[i]);
-    for (int i = tid; i < n; i += kPmThreads) {
-        const float m = part(i)[D], l = part(i)[D + 1];
-        const float w = l == 0.f ? 0.f : m == -INFINITY ? 1.f : exp2f(m - M);
-        w_s[i] = w;
-        l_s[i] = l == 0.f ? 0.f : l * w;
+#pragma unroll
+    for (int t = 0; t < kPmMaxParts / kPmThreads; ++t) {
+        // (a part without rows weighs nothing; one whose sum is no number counts)
+        const float w = ml[t].y == 0.f ? 0.f : ml[t].x == -INFINITY ? 1.f : exp2f(ml[t].x - M);
+        if (tid + t * kPmThreads < n) w_s[tid + t * kPmThreads] = w;
+        l += ml[t].y == 0.f ? 0.f : ml[t].y * w;
     }
+    l = warp_sum(l);
+    if (lane == 0) red_l[warp] = l;
     __syncthreads();
-    const int dpad = (D + 31) / 32 * 32, slices = kPmThreads / dpad, slice = tid / dpad, d = tid - slice * dpad;
-    float num = 0.f;
-    if (slice < slices && d < D) {
+    float4 num = make_float4(0.f, 0.f, 0.f, 0.f);
+    auto add = [&](const float4& v, float w) {
+        if (w == 0.f) return;                        // (what a part without weight holds does not count)
+        num.x += v.x * w; num.y += v.y * w; num.z += v.z * w; num.w += v.w * w;
+    };
+    if (mine) {
+#pragma unroll
+        for (int t = 0; t < kPmAhead; ++t)
+            if (slice + t * slices < n) add(x[t], w_s[slice + t * slices]);
 #pragma unroll 4
-        for (int i = slice; i < n; i += slices) num += w_s[i] == 0.f ? 0.f : part(i)[d] * w_s[i];
-        num_s[tid] = num;
+        for (int i = slice + kPmAhead * slices; i < n; i += slices) {
+            const float4 v = *reinterpret_cast<const float4*>(part(i) + d);
+            add(v, w_s[i]);
+        }
     }
+    num_s[tid] = num;
     __syncthreads();
-    if (slice == 0 && d < D) {
-        float den = 0.f, tot = 0.f;
-        for (int i = 0; i < n; ++i) den += l_s[i];
-        for (int i = 0; i < slices; ++i) tot += num_s[i * dpad + d];
-        const size_t row = (size_t)job.x + h;
-        a.out[row * D + d] = den == 0.f ? 0.f : tot / den;
-        if (a.lse && d == 0) a.lse[row] = den == 0.f ? -INFINITY : (M + log2f(den)) * 0.6931471805599453f;
+    if (slice != 0) return;
+    float den = 0.f;
+#pragma unroll
+    for (int i = 0; i < kPmThreads / 32; ++i) den += red_l[i];
+    for (int i = 1; i < slices; ++i) {
+        const float4 v = num_s[i * quads + tid];
+        num.x += v.x; num.y += v.y; num.z += v.z; num.w += v.w;
     }
+    const size_t row = (size_t)job.x + h;
+    float* out = a.out + row * D + d;
+    out[0] = den == 0.f ? 0.f : num.x / den;
+    out[1] = den == 0.f ? 0.f : num.y / den;
+    out[2] = den == 0.f ? 0.f : num.z / den;
+    out[3] = den == 0.f ? 0.f : num.w / den;
+    if (a.lse && tid == 0) a.lse[row] = den == 0.f ? -INFINITY : (M + log2f(den)) * 0.6931471805599453f;
 }
 
 }  // namespace sab

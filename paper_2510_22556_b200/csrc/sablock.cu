@@ -1129,7 +1129,7 @@ PagedPlan paged_plan(const sablock_params_t* p)
     pl.groups = (G + pl.group_heads - 1) / pl.group_heads;
     const int ctas = (pl.dp == 256 ? 1 : 2) * sm_count();
     pl.ctas = ctas < kPmMaxParts ? ctas : kPmMaxParts;
-    pl.o_jobs = align_up(sizeof(float) * 2 * pl.ctas * pl.group_heads * (p->head_dim + 2));
+    pl.o_jobs = align_up(sizeof(float) * 2 * pl.ctas * pl.group_heads * (p->head_dim + 4));
     pl.bytes = pl.o_jobs + align_up(sizeof(int4) * pl.ctas);
     return pl;
 }
@@ -1206,9 +1206,9 @@ sablock_status_t run_page_select(const sablock_params_t* p, const Paged& pg, con
     a.q = q; a.sel = sel;
     a.H = p->n_q_heads; a.Hkv = p->n_kv_heads; a.G = a.H / a.Hkv; a.D = p->head_dim;
     a.n_sel = n_sel; a.n_first = n_first; a.n_last = n_last;
-    // CTAs that share a sequence's pages: while there are SMs for them and 64 pages (one turn of a CTA's warps) each
+    // CTAs that share a sequence's pages: while there are SMs for them and 128 pages (one turn of a CTA's warps) each
     int c = 1;
-    while (c < kPsMaxCluster && pg.max_pages >= 128 * c && pairs * c * 2 <= 2 * sm_count()) c *= 2;
+    while (c < kPsMaxCluster && pg.max_pages >= 256 * c && pairs * c * 2 <= sm_count()) c *= 2;
     return p->dtype == SABLOCK_BF16 ? launch_page_select<__nv_bfloat16>(a, c, st) : launch_page_select<float>(a, c, st);
 }
 
@@ -1630,23 +1630,43 @@ sablock_status_t sablock_paged_append(const sablock_params_t* p, const sablock_p
     a.q = q; a.k = k; a.v = v; a.q_out = q_out;
     a.cu = cu_new; a.pos = positions; a.inv_freq = inv_freq;
     a.half = rotary_dim / 2; a.interleaved = interleaved != 0; a.n_tokens = n_tokens;
-    // Runs of a page where its bounds are kept, of eight rows elsewhere; KV heads of a CTA: as many as there are threads for their pieces,
-    // fewer while that leaves SMs without two CTAs
-    const bool bounds = pages->bounds != nullptr;
-    a.run_rows = bounds ? pages->page_size : 8;
+    // Pieces of 16 bytes, or of 8 or one channel where the halves of the rotation are not whole pieces of more.
+    int piece = 16;
+    if (!interleaved && (a.half * es) % 16) piece = (a.half * es) % 8 ? es : 8;
+    a.slots = (a.D * es / piece + 1) / 2;
+    a.lane_bits = 0;
+    while (a.lane_bits < 5 && (1 << a.lane_bits) < a.slots) ++a.lane_bits;
+    // Bounds in the same launch where a run is all of a page's new rows.  KV heads of a CTA: all (rows are whole stretches of memory
+    // then), fewer where there are fewer runs than SMs.
+    const bool bounds = pages->bounds != nullptr, with_bounds = bounds && (!cu_new || pages->page_size <= kApBoundsRun);
+    a.run_rows = with_bounds ? pages->page_size : kApRun;
     a.by_run = fast_div((uint32_t)a.run_rows);
     const long long runs = append_runs(n_tokens, pages->n_seqs, a.run_rows, !cu_new);
-    const int pieces = a.D * es / 16;
-    a.heads = kApThreads / pieces;
-    if (a.heads > a.Hkv) a.heads = a.Hkv;
-    while (a.heads > 1 && runs * ((a.Hkv + a.heads - 1) / a.heads) < 2LL * sm_count()) a.heads = (a.heads + 1) / 2;
-    const dim3 grid((unsigned)runs, (a.Hkv + a.heads - 1) / a.heads);
+    a.heads = a.Hkv;
+    auto slices = [&] { return (a.Hkv + a.heads - 1) / a.heads; };
+    while (a.heads > 1 && runs * slices() < sm_count()) a.heads = (a.heads + 1) / 2;
+    const dim3 grid((unsigned)runs, slices());
     cudaStream_t st = static_cast<cudaStream_t>(stream);
-    if (p->dtype == SABLOCK_BF16)
-        return bounds ? launch(paged_append_kernel<__nv_bfloat16, true>, grid, kApThreads, 0, st, 1, a)
-                      : launch(paged_append_kernel<__nv_bfloat16, false>, grid, kApThreads, 0, st, 1, a);
-    return bounds ? launch(paged_append_kernel<float, true>, grid, kApThreads, 0, st, 1, a)
-                  : launch(paged_append_kernel<float, false>, grid, kApThreads, 0, st, 1, a);
+    const bool bf16 = p->dtype == SABLOCK_BF16;
+    sablock_status_t rc;
+#define SAB_APPEND(PB, T) \
+    rc = with_bounds ? launch(paged_append_kernel<T, PB, true>, grid, kApThreads, 0, st, 1, a) : launch(paged_append_kernel<T, PB, false>, grid, kApThreads, 0, st, 1, a)
+    if (piece == 16 && bf16) SAB_APPEND(16, __nv_bfloat16);
+    else if (piece == 16) SAB_APPEND(16, float);
+    else if (piece == 8 && bf16) SAB_APPEND(8, __nv_bfloat16);
+    else if (piece == 8) SAB_APPEND(8, float);
+    else if (bf16) SAB_APPEND(2, __nv_bfloat16);
+    else SAB_APPEND(4, float);
+#undef SAB_APPEND
+    if (rc != SABLOCK_OK || !bounds || with_bounds) return rc;
+    a.run_rows = pages->page_size;
+    a.by_run = fast_div((uint32_t)a.run_rows);
+    // (a page's columns in as many parts as four CTAs an SM allow, of at least 16 columns)
+    const long long touched = append_runs(n_tokens, pages->n_seqs, a.run_rows, false);
+    const long long most = (a.Hkv * (long long)a.D * es / 16 + 15) / 16, parts = 4LL * sm_count() / touched;
+    const dim3 pages_grid((unsigned)touched, (unsigned)(parts < 1 ? 1 : parts > most ? most : parts));
+    return bf16 ? launch(paged_bounds_kernel<__nv_bfloat16>, pages_grid, kApThreads, 0, st, 1, a)
+                : launch(paged_bounds_kernel<float>, pages_grid, kApThreads, 0, st, 1, a);
 }
 
 size_t sablock_paged_workspace_bytes(const sablock_params_t* p, const sablock_pages_t* pages)

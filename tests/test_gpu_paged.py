@@ -65,7 +65,7 @@ def test_append(H, Hkv, D, dtype, rotary, interleaved, page, new, old, layout, b
     q_out = torch.full((total + pad, H, D), 7.0, dtype=dtype, device="cuda")
     p = _params(H, Hkv, D, dtype)
     assert B.paged_append(p, c.handle(p), k, v, q=q, positions=pos, inv_freq=freq, interleaved=interleaved, cu_new=cu, q_out=q_out) is q_out
-    assert B.last_launch_count() == 1
+    assert B.last_launch_count() == (2 if bounds and new and page > 32 else 1)
     size = R.rotate(qkv.abs(), torch.zeros_like(pos), freq, interleaved)
     if rotary:
         i = torch.arange(rotary // 2, device="cuda")
@@ -340,7 +340,7 @@ def _decode_loop(steps, graph):
     # what was moved is what decoding over the compacted cache sees
     q = torch.randn(3, H, D, generator=cs[0].g, device="cuda").to(BF16)
     a = B.decode_attention(p, q, comp.out_k[0], comp.out_v[0], n_valid=kept)
-    assert float((a - B.paged_attention(p, handles[0], q)).abs().max()) <= 4e-5 * float(comp.out_v.float().abs().max())
+    assert float((a - B.paged_attention(p, handles[0], q)).abs().max()) <= 4e-5 * float(b.v.float().abs().max())      # (rows of out_v behind n_keep hold anything)
 
     qkv = torch.empty(n_layers, 3, H + 2 * Hkv, D, dtype=BF16, device="cuda")
     pos = torch.tensor(lens, dtype=torch.int32, device="cuda") - 1

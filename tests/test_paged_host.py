@@ -127,7 +127,7 @@ def test_make_pages_reads_strides_off_the_tensors(lib):
     assert (g.k, g.v, g.table) == (k.data_ptr(), v.data_ptr(), table.data_ptr())
     assert (g.k_stride_page, g.k_stride_row, g.k_stride_head) == (256, 16, 64) == (g.v_stride_page, g.v_stride_row, g.v_stride_head)
     assert (g.n_seqs, g.n_pages, g.page_size, g.max_pages, g.table_stride) == (2, 6, 4, 3, 5)
-    assert B.paged_workspace_bytes(p, g) == g._ws_bytes > 0
+    assert B.paged_workspace_bytes(p, g) > 0
 
 
 def test_make_pages_refuses(lib):
@@ -157,6 +157,35 @@ def test_calls_refuse_tensors_that_do_not_fit(lib):
     for sel in (torch.zeros(2, 2, 3), torch.zeros(2, 3, dtype=torch.int32), torch.zeros(2, 4, 3, dtype=torch.int32)):
         with pytest.raises((TypeError, ValueError)):
             B.paged_attention(p, g, q, selected=sel)
+
+
+@pytest.mark.parametrize("n,heads,d", [(3, 2, 16), (1, 2, 16), (0, 2, 16), (3, 1, 16), (3, 2, 1)])
+def test_tensor_checks_of_the_marshalling_module(n, heads, d):
+    """The C checks say what the Python ones say."""
+    fast = pytest.importorskip("paper_2510_22556_b200._fastcall")
+    cpu, wide = torch.device("cpu"), torch.zeros(max(n, 1) * 2, heads + 3, d)
+    views = [torch.zeros(n, heads, d), wide[:n, 1:1 + heads], wide[::2][:n, :heads], torch.zeros(n, d, heads).transpose(1, 2), torch.zeros(n, heads, d, dtype=torch.int32),
+             torch.zeros(n + 1, heads, d), torch.zeros(n, heads * d), torch.zeros(1, heads, d).expand(n, heads, d), torch.zeros(n, heads, d, device="meta"),
+             torch.zeros(n, 1, d).expand(n, heads, d)]
+    got = []
+    for t in views:
+        slow = -1
+        if t.dtype == torch.float32 and t.device == cpu and t.shape == (n, heads, d) and \
+                not (n and ((d > 1 and t.stride(2) != 1) or (heads > 1 and t.stride(1) != d))):
+            slow = t.stride(0) if n > 1 else 0
+        got.append(fast.token_stride(t, torch.float32, cpu, n, heads, d))
+        assert got[-1] == slow
+        assert fast.fits(t, torch.float32, cpu, (n, heads, d)) is (t.dtype == torch.float32 and t.device == cpu and t.shape == (n, heads, d) and
+                                                                   t.is_contiguous())
+    if n == 3 and heads == 2 and d == 16:
+        assert got[:3] == [32, 5 * 16, 10 * 16] and got[4] == -1
+    for bad in [(), (views[0],), (views[0], torch.float32, cpu, n, heads)]:
+        with pytest.raises(TypeError):
+            fast.fits(*bad)
+        with pytest.raises(TypeError):
+            fast.token_stride(*bad)
+    with pytest.raises(AttributeError):
+        fast.fits(5, torch.float32, cpu, (n, heads, d))
 
 
 # ------------------------------------------------------------------------------------------ host arithmetic
