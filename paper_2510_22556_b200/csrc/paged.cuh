@@ -487,7 +487,12 @@ constexpr int kPsThreads = 512;
 constexpr int kPsWarps = kPsThreads / 32;
 constexpr int kPsBinBits = 10, kPsBins = 1 << kPsBinBits;
 constexpr int kPsMaxPages = 49152;                                 // keys of a sequence in shared memory (192 KB)
-constexpr int kPsMaxCluster = 8;
+#ifndef SAB_PS_MAXC
+#define SAB_PS_MAXC 8
+#define SAB_PS_PAGES 256
+#define SAB_PS_FILL 2
+#endif
+constexpr int kPsMaxCluster = SAB_PS_MAXC;
 constexpr uint32_t kKeyForced = 0xffffffffu, kKeyNan = 0xfffffffeu;
 
 struct PageSelectArgs {

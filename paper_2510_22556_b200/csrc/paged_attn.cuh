@@ -4,7 +4,10 @@
 // has a fixed order.  What differs:
 //
 // The lengths are on the device and ragged, so the host cannot cut the work.  A pair (sequence, KV head) has its rows in units; the
-// units of all pairs in order are one line, which the grid (as many CTAs as the device holds at once) cuts into equal shares.
+// units of all pairs of a column of KV heads (heads column, column + columns, ...) in order are one line, which its CTAs (the grid is as
+// many as the device holds at once, those of neighbouring columns neighbours) cut into equal shares.  So the CTAs of the columns go
+// along the same rows side by side, and what they read of a row at a time is a stretch of memory: with the heads one after the other
+// instead a batch of 64 sequences of 1K rows took 66 us, ATTEND_BATCH_NEW with eight columns.
 // A CTA adds the lengths up to find its share, which may start inside a pair, hold several pairs and end inside one.  Pairs that lie
 // in one share are written out; of the others every share leaves (accumulator, maximum, sum) in scratch, at most one at its
 // start and one at its end, and paged_merge_kernel, one block per share and head, adds up the pairs that begin in its share.
@@ -24,11 +27,12 @@ struct PagedAttnArgs {
     const int* sel;                                  // [n_seqs][Hkv][n_sel], or NULL: all pages
     int n_sel;
     int H, Hkv, G, D;
+    int columns;                                     // of KV heads (and their groups), a divisor of Hkv * groups and of the grid
     int groups, group_heads;                         // head groups of a KV head, heads of a group (the last may have fewer)
     bool same_place;                                 // K and V have the same strides
     float c2;                                        // log2(e) / sqrt(D)
     float* part;                                     // [2 x CTAs][group_heads][D + 4]: accumulator, max (log2 units), sum
-    int4* jobs;                                      // [CTAs]: first head row, heads, parts
+    int4* jobs;                                      // [CTAs]: first head row, heads, parts (every columns-th CTA from this one on)
     float* out;                                      // [n_seqs][H][D]
     float* lse;                                      // optional [n_seqs][H]
     // rows of sequence s that the queries see through the list (a last page's absent rows count)
@@ -39,7 +43,8 @@ struct PagedAttnArgs {
     }
 };
 
-// A CTA's share [u, u_end) of the line of units; where it starts: sequence s, `skip` units into the units of that sequence's pairs.
+// A CTA's share [u, u_end) of its column's line of units; where it starts: sequence s, `skip` units into the units of that
+// sequence's pairs of the column.
 struct PgShare {
     long long u, u_end, quota, skip;
     int s;
@@ -73,8 +78,9 @@ __device__ __forceinline__ PgShare pg_share(const PagedAttnArgs& a, int pairs)
     }
     total *= pairs;
     PgShare r;
-    r.quota = (total + gridDim.x - 1) / gridDim.x;
-    r.u = min((long long)blockIdx.x * r.quota, total);
+    const int shares = gridDim.x / a.columns;
+    r.quota = (total + shares - 1) / shares;
+    r.u = min((long long)(blockIdx.x / a.columns) * r.quota, total);
     r.u_end = min(r.u + r.quota, total);
     long long before = (upto - mine) * pairs;
     if (r.u >= before && r.u < before + mine * pairs)
@@ -93,7 +99,7 @@ __device__ __forceinline__ PgShare pg_share(const PagedAttnArgs& a, int pairs)
     return r;
 }
 
-// Walks the pairs of a share: the segment of the pair that is in it.
+// The segment of pair `pair` of sequence s (of those of the column) from unit w on, of which `left` units are the share's.
 struct PgSegment {
     int s, hk, g0, heads;                            // sequence, KV head, first head of the group, heads
     int rows, row0, row1;                            // rows of the pair, and the segment's
@@ -101,17 +107,18 @@ struct PgSegment {
     long long units;                                 // of the pair
 };
 template <int UNIT>
-__device__ __forceinline__ PgSegment pg_segment(const PagedAttnArgs& a, const PgShare& sh, int s, int pair, int w)
+__device__ __forceinline__ PgSegment pg_segment(const PagedAttnArgs& a, int s, int pair, int w, long long left)
 {
     PgSegment g;
     g.s = s;
+    pair = pair * a.columns + (int)blockIdx.x % a.columns;
     g.hk = pair / a.groups;
     const int gi = pair - g.hk * a.groups;
     g.g0 = gi * a.group_heads;
     g.heads = min(a.group_heads, a.G - g.g0);
     g.rows = a.listed_rows(s);
     g.units = max(1, (g.rows + UNIT - 1) / UNIT);
-    const long long n = min(g.units - w, sh.u_end - sh.u);
+    const long long n = min(g.units - w, left);
     g.first = w == 0;
     g.last = w + n == g.units;
     g.row0 = w * UNIT;
@@ -182,6 +189,23 @@ __device__ __forceinline__ void pg_emit(const PagedAttnArgs& a, const PgSegment&
     }
 }
 
+__device__ __forceinline__ void pg_emit4(const PagedAttnArgs& a, const PgSegment& g, int h, int d, const float4& sum, float m, float l)
+{
+    if (g.first && g.last) {
+        const size_t row = pg_head(a, g) + h;
+        float* dst = a.out + row * a.D + d;
+        dst[0] = l == 0.f ? 0.f : sum.x / l;
+        dst[1] = l == 0.f ? 0.f : sum.y / l;
+        dst[2] = l == 0.f ? 0.f : sum.z / l;
+        dst[3] = l == 0.f ? 0.f : sum.w / l;
+        if (a.lse && d == 0) a.lse[row] = l == 0.f ? -INFINITY : (m + log2f(l)) * 0.6931471805599453f;
+    } else {
+        float* dst = pg_part(a, g, h);
+        *reinterpret_cast<float4*>(dst + d) = sum;
+        if (d == 0) *reinterpret_cast<float2*>(dst + a.D) = make_float2(m, l);
+    }
+}
+
 // ---- bf16 -----------------------------------------------------------------------------------------------
 // As decode_mma_kernel (decode.cuh has the reasons): four warps, each with a private ring of 16-row chunks and its own online
 // softmax; a unit is 64 rows.  Up to four heads (Q4) go into rows 0-3 of the 16-row A operand and again into rows 4-7: rows 0-3
@@ -194,7 +218,10 @@ constexpr int kPaThreads = 128;
 constexpr int kPaWarps = kPaThreads / 32;
 constexpr int kPaStages = 3;
 constexpr int kPaUnit = 16 * kPaWarps;
-__host__ __device__ constexpr int pa_smem(int DP) { return kPaWarps * kPaStages * 2 * 16 * DP * 2; }
+__host__ __device__ constexpr int pa_ring_bytes(int DP) { return kPaWarps * kPaStages * 2 * 16 * DP * 2; }
+// the ring, the sums of the warps for four heads, the queries (a row of heads' channels is 16 bytes longer: eight rows fall into all banks)
+__host__ __device__ constexpr int pa_smem(int DP, int heads) { return pa_ring_bytes(DP) + kPaWarps * 4 * DP * (int)sizeof(float) + heads * (DP + 8) * 2; }
+static_assert(2 * (pa_smem(128, 16) + 512 + 1024) <= kSmSharedBytes, "two CTAs on an SM");
 
 template <int NS, bool Q4, int DP>
 __global__ void __launch_bounds__(kPaThreads, DP == 256 ? 1 : 2)
@@ -204,15 +231,18 @@ paged_mma_kernel(const __grid_constant__ PagedAttnArgs a)
     constexpr int PR = DP / 8;                       // 16-byte pieces of a row
     constexpr int KS = DP / 16;                      // k-steps of the logits
     constexpr int GP = Q4 ? 4 : 8 * NS;              // heads of a group
+    constexpr int kQn = (GP * PR + kPaThreads - 1) / kPaThreads;
     constexpr uint32_t kOp = 16 * DP * 2;            // bytes of a chunk of K or V
     using bf16 = __nv_bfloat16;
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     extern __shared__ __align__(128) uint8_t pa_ring[];
-    __shared__ float ms[kPaWarps][GP], ls[kPaWarps][GP];
+    float (*accs)[4][DP] = reinterpret_cast<float (*)[4][DP]>(pa_ring + pa_ring_bytes(DP));
+    bf16 (*qs)[DP + 8] = reinterpret_cast<bf16 (*)[DP + 8]>(pa_ring + pa_ring_bytes(DP) + kPaWarps * 4 * DP * sizeof(float));
+    __shared__ float ms[kPaWarps][4], ls[kPaWarps][4];
     const uint32_t ring = smem_u32(pa_ring) + warp * kPaStages * 2 * kOp;
     pdl_wait();
     pdl_launch();
-    const int pairs = a.Hkv * a.groups;
+    const int pairs = a.Hkv * a.groups / a.columns;  // of a sequence in this CTA's column
     PgShare sh = pg_share<kPaThreads, kPaUnit>(a, pairs);
     if (tid == 0) a.jobs[blockIdx.x] = make_int4(0, 0, 0, 0);
     if (sh.u >= sh.u_end) return;
@@ -222,70 +252,124 @@ paged_mma_kernel(const __grid_constant__ PagedAttnArgs a)
         pair = (int)(sh.skip / units);
         w = (int)(sh.skip - pair * units);
     }
-    const int n_pieces = a.D / 8;
-    while (sh.u < sh.u_end) {
-        const PgSegment g = pg_segment<kPaUnit>(a, sh, s, pair, w);
-        const PgLook look = pg_look(a, g);
-        const int chunks = g.row1 > g.row0 ? (g.row1 - g.row0 + 15) / 16 : 0;
-        const int n_it = (chunks - warp + kPaWarps - 1) / kPaWarps;
-        const bf16* kb = static_cast<const bf16*>(a.pg.k) + (size_t)g.hk * a.pg.k_head;
-        const bf16* vb = static_cast<const bf16*>(a.pg.v) + (size_t)g.hk * a.pg.v_head;
-        const int pc = lane % PR;
-        const bool piece_there = pc < n_pieces;
+    const int n_pieces = a.D / 8, pc = lane % PR;
+    const bool piece_there = pc < n_pieces;
+    const int lr = lane & 7, mat = lane >> 3;
+    auto chunks_of = [&](const PgSegment& g) { return ((g.row1 > g.row0 ? (g.row1 - g.row0 + 15) / 16 : 0) - warp + kPaWarps - 1) / kPaWarps; };
 
-        // this lane's row of the warp's chunk `it`
-        auto row_of = [&](int it) { return g.row0 + (it * kPaWarps + warp) * 16 + (lane & 15); };
-        auto listed = [&](int it) { return pg_listed(a, look, row_of(it)); };
-        auto find = [&](int it, int j) { return pg_find(a, look, row_of(it), j); };
-        auto issue = [&](int it, const PgRow r) {
-            if (it < n_it) {
-                const uint32_t dst = ring + (uint32_t)(it % kPaStages) * 2 * kOp;
-                const bool ok = r.ok && a.pg.holds(r.page);
-                const long long ko = ok ? (long long)r.page * a.pg.k_page + (long long)r.slot * a.pg.k_row : -1;
-                const long long vo = a.same_place ? ko : ok ? (long long)r.page * a.pg.v_page + (long long)r.slot * a.pg.v_row : -1;
-#pragma unroll
-                for (int i = 0; i < PR / 2; ++i) {
-                    const int rr = lane / PR + i * (32 / PR);
-                    const long long k_at = __shfl_sync(0xffffffffu, ko, rr);
-                    const long long v_at = a.same_place ? k_at : __shfl_sync(0xffffffffu, vo, rr);
-                    const bool there = k_at >= 0 && piece_there;
-                    const uint32_t o = dst + (uint32_t)(rr * PR + (pc ^ (rr & 7))) * 16;
-                    cp_async16_or_zero(o, kb + (there ? k_at + pc * 8 : 0), there);
-                    cp_async16_or_zero(o + kOp, vb + (there ? v_at + pc * 8 : 0), there);
-                }
-            }
-            cp_async_commit();
-        };
-        // copies of chunk it + kPaStages - 1 go out at chunk it; its rows have been looked up one turn, its pages two turns earlier
-        uint32_t there_ring[kPaStages - 1];          // which rows of the chunks in flight exist, a bit each
-        {
-            PgRow r[kPaStages - 1];
-            int j[kPaStages - 1];
-#pragma unroll
-            for (int t = 0; t < kPaStages - 1; ++t) j[t] = listed(t);
-#pragma unroll
-            for (int t = 0; t < kPaStages - 1; ++t) r[t] = find(t, j[t]);
-#pragma unroll
-            for (int t = 0; t < kPaStages - 1; ++t) {
-                there_ring[t] = __ballot_sync(0xffffffffu, r[t].ok && a.pg.holds(r[t].page)) & 0xffffu;
-                issue(t, r[t]);
-            }
+    // The copies: a cursor of its own, kPaStages - 1 chunks ahead of the products and over the ends of segments, so that the loads of the
+    // next segment are on their way while one is merged.  A chunk's rows are looked up one chunk, their pages two chunks earlier.
+    struct {
+        long long left;                              // units of the share that are not opened
+        int s, pair, w;
+        int k, n;                                    // next chunk of this warp in the open segment, and its chunks
+        int stage;
+    } io = {sh.u_end - sh.u, s, pair, w, 0, 0, 0};
+    PgSegment g;
+    PgLook look;
+    const bf16 *kb, *vb;
+    int io_row;                                      // this lane's row of the open segment's chunk 0
+    PgRow next;
+    int next_j;
+    uint32_t there_ring = 0;                         // which rows of the chunks in flight exist, 16 bits each, the newest on top
+    static_assert(kPaStages == 3, "two chunks in flight beside the one at hand");
+    auto open = [&] {                                // the next segment that has chunks for this warp
+        while (io.k == io.n && io.left > 0) {
+            const PgSegment g = pg_segment<kPaUnit>(a, io.s, io.pair, io.w, io.left);
+            io.left -= min(g.units - io.w, io.left);
+            io.w = 0;
+            if (++io.pair == pairs) { io.pair = 0; ++io.s; }
+            io.k = 0;
+            io.n = chunks_of(g);
+            if (io.n == 0) continue;
+            look = pg_look(a, g);
+            kb = static_cast<const bf16*>(a.pg.k) + (size_t)g.hk * a.pg.k_head;
+            vb = static_cast<const bf16*>(a.pg.v) + (size_t)g.hk * a.pg.v_head;
+            io_row = g.row0 + warp * 16 + (lane & 15);
+            const int j = pg_listed(a, look, io_row);
+            next_j = pg_listed(a, look, io_row + kPaUnit);
+            next = pg_find(a, look, io_row, j);
         }
-        PgRow next = find(kPaStages - 1, listed(kPaStages - 1));
-        int next_j = listed(kPaStages);
-
-        uint32_t qa[KS][2 * NS];
+    };
+    auto step = [&] {
+        uint32_t there_rows = 0;
+        if (io.k < io.n) {
+            const uint32_t dst = ring + (uint32_t)io.stage * 2 * kOp;
+            const bool ok = next.ok && a.pg.holds(next.page);
+            const long long ko = ok ? (long long)next.page * a.pg.k_page + (long long)next.slot * a.pg.k_row : -1;
+            const long long vo = a.same_place ? ko : ok ? (long long)next.page * a.pg.v_page + (long long)next.slot * a.pg.v_row : -1;
+            there_rows = __ballot_sync(0xffffffffu, ok) & 0xffffu;
+#pragma unroll
+            for (int i = 0; i < PR / 2; ++i) {
+                const int rr = lane / PR + i * (32 / PR);
+                const long long k_at = __shfl_sync(0xffffffffu, ko, rr);
+                const long long v_at = a.same_place ? k_at : __shfl_sync(0xffffffffu, vo, rr);
+                const bool there = k_at >= 0 && piece_there;
+                const uint32_t o = dst + (uint32_t)(rr * PR + (pc ^ (rr & 7))) * 16;
+                cp_async16_or_zero(o, kb + (there ? k_at + pc * 8 : 0), there);
+                cp_async16_or_zero(o + kOp, vb + (there ? v_at + pc * 8 : 0), there);
+            }
+            ++io.k;
+            next = pg_find(a, look, io_row + io.k * kPaUnit, next_j);
+            next_j = pg_listed(a, look, io_row + (io.k + 1) * kPaUnit);
+            io.stage = io.stage == kPaStages - 1 ? 0 : io.stage + 1;
+            open();                                  // (its look-ups are on their way until the next step)
+        }
+        there_ring = there_ring >> 16 | there_rows << 16;
+        cp_async_commit();
+    };
+    // The queries of a segment: asked for while the segment before is worked on, put into shared memory at its end, then taken as
+    // fragments by every warp.
+    uint4 q_next[kQn];
+    auto ask_queries = [&](const PgSegment& g) {
+#pragma unroll
+        for (int t = 0; t < kQn; ++t) {
+            const int i = tid + t * kPaThreads, h = min(i / PR, g.heads - 1), c = min(i % PR, n_pieces - 1);
+            q_next[t] = *reinterpret_cast<const uint4*>(static_cast<const bf16*>(a.q) + (pg_head(a, g) + h) * a.D + c * 8);
+        }
+    };
+    auto put_queries = [&] {
+#pragma unroll
+        for (int t = 0; t < kQn; ++t) {
+            const int i = tid + t * kPaThreads;
+            if (i < GP * PR) *reinterpret_cast<uint4*>(&qs[i / PR][i % PR * 8]) = i % PR < n_pieces ? q_next[t] : make_uint4(0, 0, 0, 0);
+        }
+    };
+    uint32_t qa[KS][2 * NS];
+    auto take_queries = [&] {
 #pragma unroll
         for (int n = 0; n < NS; ++n) {
             const int hh = Q4 ? (lane >> 2) & 3 : 8 * n + (lane >> 2);
-            const bf16* qg = static_cast<const bf16*>(a.q) + (pg_head(a, g) + min(hh, g.heads - 1)) * a.D + 2 * (lane & 3);
 #pragma unroll
             for (int ks = 0; ks < KS; ++ks)
 #pragma unroll
-                for (int x = 0; x < 2; ++x) {
-                    const int d = ks * 16 + x * 8;
-                    qa[ks][2 * n + x] = d < a.D ? *reinterpret_cast<const uint32_t*>(qg + d) : 0u;
-                }
+                for (int x = 0; x < 2; ++x)
+                    qa[ks][2 * n + x] = *reinterpret_cast<const uint32_t*>(&qs[hh][ks * 16 + x * 8 + 2 * (lane & 3)]);
+        }
+    };
+    // segment after the one at hand
+    auto advance = [&] {
+        sh.u += min(g.units - w, sh.u_end - sh.u);
+        w = 0;
+        if (++pair == pairs) { pair = 0; ++s; }
+    };
+    int stage = 0;
+    g = pg_segment<kPaUnit>(a, s, pair, w, sh.u_end - sh.u);
+    ask_queries(g);
+    open();
+    step();
+    step();
+    put_queries();
+    __syncthreads();
+    while (true) {
+        take_queries();
+        const PgSegment at = g;                      // the segment at hand; g is the next one from here on
+        const long long unit = sh.u;
+        advance();
+        const bool more = sh.u < sh.u_end;
+        if (more) {
+            g = pg_segment<kPaUnit>(a, s, pair, w, sh.u_end - sh.u);
+            ask_queries(g);
         }
         float m[NS], l[NS], acc[NS][DP / 8][4];
 #pragma unroll
@@ -297,18 +381,14 @@ paged_mma_kernel(const __grid_constant__ PagedAttnArgs a)
 #pragma unroll
                 for (int e = 0; e < 4; ++e) acc[n][i][e] = 0.f;
         }
-        const int lr = lane & 7, mat = lane >> 3;
+        const int n_it = chunks_of(at);
         for (int it = 0; it < n_it; ++it) {
-            const uint32_t there = there_ring[0];
-#pragma unroll
-            for (int t = 0; t + 1 < kPaStages - 1; ++t) there_ring[t] = there_ring[t + 1];
-            there_ring[kPaStages - 2] = __ballot_sync(0xffffffffu, next.ok && a.pg.holds(next.page)) & 0xffffu;
-            issue(it + kPaStages - 1, next);
-            next = find(it + kPaStages, next_j);
-            next_j = listed(it + kPaStages + 1);
+            const uint32_t there = there_ring & 0xffffu;         // (of the two chunks in flight, the older one)
+            step();
             cp_async_wait<kPaStages - 1>();
             __syncwarp();
-            const uint32_t ks_base = ring + (uint32_t)(it % kPaStages) * 2 * kOp, vs_base = ks_base + kOp;
+            const uint32_t ks_base = ring + (uint32_t)stage * 2 * kOp, vs_base = ks_base + kOp;
+            stage = stage == kPaStages - 1 ? 0 : stage + 1;
             float c[2][4];
 #pragma unroll
             for (int x = 0; x < 2; ++x)
@@ -387,58 +467,60 @@ paged_mma_kernel(const __grid_constant__ PagedAttnArgs a)
             }
             __syncwarp();                            // the stage may be refilled
         }
-        cp_async_wait<0>();
-        __syncthreads();
-        // ---- merge: the pieces, then the warps (over the ring), in a fixed order
-        float (*accs)[GP][DP] = reinterpret_cast<float (*)[GP][DP]>(pa_ring);
-        static_assert(kPaWarps * GP * DP * (int)sizeof(float) <= pa_smem(DP), "accumulators fit in the ring");
+        // The segment is over: the pieces are added and the warps merged, in a fixed order, four heads at a time.
+        if (tid == 0 && at.first && !at.last) {
+            // the pair goes on in the next shares: the last unit of it is unit `end` of the line
+            const long long end = unit + at.units - 1;
+            a.jobs[blockIdx.x] = make_int4((int)pg_head(a, at), at.heads, (int)(end / sh.quota) - (int)blockIdx.x / a.columns + 1, 0);
+        }
 #pragma unroll
         for (int n = 0; n < NS; ++n) {
-            const int hh = Q4 ? (lane >> 2) & 3 : 8 * n + (lane >> 2);
-            const bool mine = !Q4 || lane < 16;
             l[n] += __shfl_xor_sync(0xffffffffu, l[n], 1);
             l[n] += __shfl_xor_sync(0xffffffffu, l[n], 2);
+        }
+#pragma unroll
+        for (int r = 0; r < GP / 4; ++r) {
+            const int n = r / 2;
+            const bool mine = lane >> 4 == (r & 1);                // (with four heads, lanes 16 to 31 have copies)
 #pragma unroll
             for (int i = 0; i < DP / 8; ++i) {
-                float r[2];
+                float x[2];
 #pragma unroll
                 for (int e = 0; e < 2; ++e) {
                     const float less = Q4 ? acc[n][i][2 + e] + __shfl_down_sync(0xffffffffu, acc[n][i][e], 16) : acc[n][i][2 + e];
                     // an infinite value times a smaller piece is an infinity of either sign or, where the piece is zero, no
                     // number: the leading piece alone says what the weight times the value is
-                    r[e] = isinf(acc[n][i][e]) ? acc[n][i][e] : acc[n][i][e] + less;
+                    x[e] = isinf(acc[n][i][e]) ? acc[n][i][e] : acc[n][i][e] + less;
                 }
-                if (mine) *reinterpret_cast<float2*>(&accs[warp][hh][i * 8 + 2 * (lane & 3)]) = make_float2(r[0], r[1]);
+                if (mine) *reinterpret_cast<float2*>(&accs[warp][(lane >> 2) & 3][i * 8 + 2 * (lane & 3)]) = make_float2(x[0], x[1]);
             }
-            if (mine && (lane & 3) == 0) { ms[warp][hh] = m[n]; ls[warp][hh] = l[n]; }
-        }
-        __syncthreads();
-        for (int i = tid; i < g.heads * a.D; i += kPaThreads) {
-            const int h = i / a.D, d = i - h * a.D;
-            float mx = -INFINITY;
+            if (mine && (lane & 3) == 0) { ms[warp][(lane >> 2) & 3] = m[n]; ls[warp][(lane >> 2) & 3] = l[n]; }
+            __syncthreads();
+            if (r == 0 && more) put_queries();           // (every warp has taken those of this segment)
 #pragma unroll
-            for (int v = 0; v < kPaWarps; ++v) mx = fmaxf(mx, ms[v][h]);
-            float sum = 0.f, lsum = 0.f;
+            for (int i = tid; i < 4 * DP / 4; i += kPaThreads) {
+                const int hs = i / (DP / 4), h = 4 * r + hs, d = 4 * (i % (DP / 4));
+                if (h >= at.heads || d >= a.D) continue;
+                float mx = -INFINITY;
 #pragma unroll
-            for (int v = 0; v < kPaWarps; ++v) {
-                if (ls[v][h] == 0.f) continue;       // (a warp without rows; one whose sum is no number counts)
-                const float wt = ms[v][h] == -INFINITY ? 1.f : exp2f(ms[v][h] - mx);
-                sum += accs[v][h][d] * wt;
-                lsum += ls[v][h] * wt;
+                for (int v = 0; v < kPaWarps; ++v) mx = fmaxf(mx, ms[v][hs]);
+                float4 sum = make_float4(0.f, 0.f, 0.f, 0.f);
+                float lsum = 0.f;
+#pragma unroll
+                for (int v = 0; v < kPaWarps; ++v) {
+                    if (ls[v][hs] == 0.f) continue;  // (a warp without rows; one whose sum is no number counts)
+                    const float wt = ms[v][hs] == -INFINITY ? 1.f : exp2f(ms[v][hs] - mx);
+                    const float4 x = *reinterpret_cast<const float4*>(&accs[v][hs][d]);
+                    sum.x += x.x * wt; sum.y += x.y * wt; sum.z += x.z * wt; sum.w += x.w * wt;
+                    lsum += ls[v][hs] * wt;
+                }
+                pg_emit4(a, at, h, d, sum, mx, lsum);
             }
-            pg_emit(a, g, h, d, sum, mx, lsum);
+            __syncthreads();                             // the sums may be written again
         }
-        if (tid == 0 && g.first && !g.last) {
-            // the pair goes on in the next shares: the last unit of it is unit `end` of the line
-            const long long end = sh.u + g.units - 1;
-            a.jobs[blockIdx.x] = make_int4((int)pg_head(a, g), g.heads, (int)(end / sh.quota) - (int)blockIdx.x + 1, 0);
-        }
-        const long long n = min(g.units - w, sh.u_end - sh.u);
-        sh.u += n;
-        w = 0;
-        if (++pair == pairs) { pair = 0; ++s; }
-        __syncthreads();                             // the ring may be filled again
+        if (!more) break;
     }
+    cp_async_wait<0>();
 }
 
 // ---- fp32 -----------------------------------------------------------------------------------------------
@@ -468,7 +550,7 @@ paged_fma_kernel(const __grid_constant__ PagedAttnArgs a)
     const uint8_t* ring_p = pa_ring + warp * kPfStages * 2 * kOp;
     pdl_wait();
     pdl_launch();
-    const int pairs = a.Hkv * a.groups;
+    const int pairs = a.Hkv * a.groups / a.columns;  // of a sequence in this CTA's column
     PgShare sh = pg_share<kPaThreads, kPfUnit>(a, pairs);
     if (tid == 0) a.jobs[blockIdx.x] = make_int4(0, 0, 0, 0);
     if (sh.u >= sh.u_end) return;
@@ -480,7 +562,7 @@ paged_fma_kernel(const __grid_constant__ PagedAttnArgs a)
     }
     const int n_pieces = a.D / 4;
     while (sh.u < sh.u_end) {
-        const PgSegment g = pg_segment<kPfUnit>(a, sh, s, pair, w);
+        const PgSegment g = pg_segment<kPfUnit>(a, s, pair, w, sh.u_end - sh.u);
         const PgLook look = pg_look(a, g);
         const int chunks = g.row1 > g.row0 ? (g.row1 - g.row0 + kPfRows - 1) / kPfRows : 0;
         const int n_it = (chunks - warp + kPaWarps - 1) / kPaWarps;
@@ -637,7 +719,7 @@ paged_fma_kernel(const __grid_constant__ PagedAttnArgs a)
         }
         if (tid == 0 && g.first && !g.last) {
             const long long end = sh.u + g.units - 1;
-            a.jobs[blockIdx.x] = make_int4((int)pg_head(a, g), g.heads, (int)(end / sh.quota) - (int)blockIdx.x + 1, 0);
+            a.jobs[blockIdx.x] = make_int4((int)pg_head(a, g), g.heads, (int)(end / sh.quota) - (int)blockIdx.x / a.columns + 1, 0);
         }
         const long long n = min(g.units - w, sh.u_end - sh.u);
         sh.u += n;
@@ -666,8 +748,8 @@ paged_merge_kernel(const __grid_constant__ PagedAttnArgs a)
     const int4 job = a.jobs[b];
     if (h >= job.y) return;
     const int n = job.z, D = a.D, quads = D / 4, slices = kPmThreads / quads, slice = tid / quads, d = 4 * (tid - slice * quads);
-    // part i: of share b + i, at its end for the first, at its start for the others
-    auto part = [&](int i) { return a.part + (((size_t)2 * (b + i) + (i == 0 ? 1 : 0)) * a.group_heads + h) * (D + 4); };
+    // part i: of the i-th share from this one on, at its end for the first, at its start for the others
+    auto part = [&](int i) { return a.part + (((size_t)2 * (b + i * a.columns) + (i == 0 ? 1 : 0)) * a.group_heads + h) * (D + 4); };
     const bool mine = slice < slices;
     float4 x[kPmAhead];
 #pragma unroll

@@ -1117,7 +1117,7 @@ sablock_status_t paged_args(const sablock_params_t* p, const sablock_pages_t* pa
 }
 
 // The kernel of a call and its scratch.
-struct PagedPlan { int group_heads, groups, dp, ctas; size_t o_jobs, bytes; };
+struct PagedPlan { int group_heads, groups, dp, columns, ctas; size_t o_jobs, bytes; };
 PagedPlan paged_plan(const sablock_params_t* p)
 {
     PagedPlan pl;
@@ -1127,8 +1127,13 @@ PagedPlan paged_plan(const sablock_params_t* p)
     const int most = p->dtype == SABLOCK_BF16 && pl.dp <= 128 ? 16 : 8;
     pl.group_heads = G <= 4 ? 4 : G <= 8 || most == 8 ? 8 : 16;
     pl.groups = (G + pl.group_heads - 1) / pl.group_heads;
-    const int ctas = (pl.dp == 256 ? 1 : 2) * sm_count();
-    pl.ctas = ctas < kPmMaxParts ? ctas : kPmMaxParts;
+    int ctas = (pl.dp == 256 ? 1 : 2) * sm_count();
+    if (ctas > kPmMaxParts) ctas = kPmMaxParts;
+    // Columns of heads: a divisor of theirs, up to 16, that leaves the fewest CTAs without work; the most columns of those
+    const int all = p->n_kv_heads * pl.groups;
+    pl.ctas = 0;
+    for (int d = all < 16 ? all : 16; d >= 1; --d)
+        if (all % d == 0 && ctas / d * d > pl.ctas) { pl.columns = d; pl.ctas = ctas / d * d; }
     pl.o_jobs = align_up(sizeof(float) * 2 * pl.ctas * pl.group_heads * (p->head_dim + 4));
     pl.bytes = pl.o_jobs + align_up(sizeof(int4) * pl.ctas);
     return pl;
@@ -1137,8 +1142,9 @@ PagedPlan paged_plan(const sablock_params_t* p)
 template <int NS, bool Q4, int DP>
 sablock_status_t launch_paged_mma(const PagedAttnArgs& a, int ctas, cudaStream_t st)
 {
-    SAB_TRY(allow_smem<paged_mma_kernel<NS, Q4, DP>>(pa_smem(DP)));
-    return launch(paged_mma_kernel<NS, Q4, DP>, dim3(ctas), kPaThreads, pa_smem(DP), st, 1, a);
+    constexpr int smem = pa_smem(DP, Q4 ? 4 : 8 * NS);
+    SAB_TRY(allow_smem<paged_mma_kernel<NS, Q4, DP>>(smem));
+    return launch(paged_mma_kernel<NS, Q4, DP>, dim3(ctas), kPaThreads, smem, st, 1, a);
 }
 template <int GP, int DP>
 sablock_status_t launch_paged_fma(const PagedAttnArgs& a, int ctas, cudaStream_t st)
@@ -1157,7 +1163,7 @@ sablock_status_t run_paged_attention(const sablock_params_t* p, const Paged& pg,
     a.pg = pg;
     a.q = q; a.sel = sel; a.n_sel = n_sel;
     a.H = p->n_q_heads; a.Hkv = p->n_kv_heads; a.G = a.H / a.Hkv; a.D = p->head_dim;
-    a.groups = pl.groups; a.group_heads = pl.group_heads;
+    a.columns = pl.columns; a.groups = pl.groups; a.group_heads = pl.group_heads;
     a.same_place = pg.k_page == pg.v_page && pg.k_row == pg.v_row;
     a.c2 = (float)(1.4426950408889634 / sqrt((double)p->head_dim));
     a.part = static_cast<float*>(ws);
@@ -1186,6 +1192,7 @@ sablock_status_t launch_page_select(const PageSelectArgs& a, int cluster, cudaSt
     const dim3 grid(cluster, a.pg.n_seqs * a.Hkv);
 #define SAB_SELECT(N) \
     do { SAB_TRY(allow_smem<page_select_kernel<T, N>>(smem)); \
+         if (cluster > 8) cudaFuncSetAttribute(page_select_kernel<T, N>, cudaFuncAttributeNonPortableClusterSizeAllowed, 1); \
          return launch(page_select_kernel<T, N>, grid, kPsThreads, smem, st, cluster, a, cluster); } while (0)
     if (per <= 1) SAB_SELECT(1);
     if constexpr (sizeof(T) == 4)
@@ -1208,7 +1215,7 @@ sablock_status_t run_page_select(const sablock_params_t* p, const Paged& pg, con
     a.n_sel = n_sel; a.n_first = n_first; a.n_last = n_last;
     // CTAs that share a sequence's pages: while there are SMs for them and 128 pages (one turn of a CTA's warps) each
     int c = 1;
-    while (c < kPsMaxCluster && pg.max_pages >= 256 * c && pairs * c * 2 <= sm_count()) c *= 2;
+    while (c < kPsMaxCluster && pg.max_pages >= SAB_PS_PAGES * c && pairs * c * 2 <= SAB_PS_FILL * sm_count()) c *= 2;
     return p->dtype == SABLOCK_BF16 ? launch_page_select<__nv_bfloat16>(a, c, st) : launch_page_select<float>(a, c, st);
 }
 
