@@ -479,20 +479,15 @@ paged_bounds_kernel(const __grid_constant__ AppendArgs a)
 // so the queries are added first and a page costs 2 D multiply-adds, whatever the number of heads.  Sums are in double, rounded
 // once to fp32: which page comes in at the border then does not hang on the order of a sum.  Ties go to the lower page.
 //
-// A cluster of CTAs has one (sequence, KV head).  Its warps score eight pages at a time (a page's bounds are one row of 4 D bytes in
-// bf16, read by the whole warp) and leave the order-preserving integer images of the scores in the shared memory of CTA 0, which
-// finds the n_sel-th largest by counting into 1024 bins over the range of the keys, then over the range of the bin that it is
-// in, until all of a bin is in or its keys are equal.
-constexpr int kPsThreads = 512;
-constexpr int kPsWarps = kPsThreads / 32;
+// A cluster of CTAs has one (sequence, KV head).  Its warps score several pages at a time (a page's bounds are one row of 4 D bytes in
+// bf16, read by the whole warp) and leave the order-preserving integer images of the scores in shared memory.  The n_sel-th largest is
+// found by counting into 1024 bins over the range of the keys, then over the range of the bin that it is in, until all of a bin is in
+// or its keys are equal.  Two kernels do this: page_select_kernel below, where CTA 0 of the cluster chooses, and
+// paged_cluster_kernel (paged_attn.cuh), where every CTA does, for itself.
+__host__ __device__ constexpr int ps_threads(int NP) { return NP > 2 ? 256 : 512; }      // (registers for eight pages)
 constexpr int kPsBinBits = 10, kPsBins = 1 << kPsBinBits;
 constexpr int kPsMaxPages = 49152;                                 // keys of a sequence in shared memory (192 KB)
-#ifndef SAB_PS_MAXC
-#define SAB_PS_MAXC 8
-#define SAB_PS_PAGES 256
-#define SAB_PS_FILL 2
-#endif
-constexpr int kPsMaxCluster = SAB_PS_MAXC;
+constexpr int kPsMaxCluster = 8;
 constexpr uint32_t kKeyForced = 0xffffffffu, kKeyNan = 0xfffffffeu;
 
 struct PageSelectArgs {
@@ -513,9 +508,12 @@ __device__ __forceinline__ void st_cluster_u32(const void* p, int rank, uint32_t
 {
     asm volatile("st.shared::cluster.u32 [%0], %1;" ::"r"(cluster_map(p, rank)), "r"(v) : "memory");
 }
+// The halves of cluster_sync: what a thread does between them need not wait for the others.
+__device__ __forceinline__ void cluster_arrive() { asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory"); }
+__device__ __forceinline__ void cluster_await() { asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory"); }
 
 // Sums of a warp's values, eight at a time: lane 4 p (p = 0 .. 7) and its three neighbours have the sum of v[p].
-__device__ __forceinline__ double sum8(double (&v)[8], int lane)
+__device__ __forceinline__ double sum8(double* v, int lane)
 {
 #pragma unroll
     for (int o = 16, n = 4; o >= 4; o >>= 1, n >>= 1) {
@@ -530,76 +528,63 @@ __device__ __forceinline__ double sum8(double (&v)[8], int lane)
     return x + __shfl_xor_sync(0xffffffffu, x, 1);
 }
 
-// NP: 16-byte pieces of a page's bounds that a lane has
-template <typename T, int NP>
-__global__ void __launch_bounds__(kPsThreads)
-page_select_kernel(const __grid_constant__ PageSelectArgs a, int n_cta)
+// Scores pages at, at + 1, .. at + NB - 1, then from at + step on, of the P pages of sequence s for KV head hk, by a warp: ready() before the
+// first result, then store(page, key), called by the four lanes that hold it.  NP: 16-byte pieces of a page's bounds that a lane has.
+template <typename T, int NP, int NB, typename Ready, typename Store>
+__device__ __forceinline__ void score_pages(const PageSelectArgs& a, int s, int hk, int P, int at, int step, Ready&& ready, Store&& store)
 {
     constexpr int E = PgVec<T>::kElems;
     const Paged& pg = a.pg;
-    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-    const int rank = blockIdx.x, pair = blockIdx.y, s = pair / a.Hkv, hk = pair - s * a.Hkv;
-    extern __shared__ __align__(16) uint32_t ps_keys[];
-    __shared__ int hist[kPsBins];
-    __shared__ int tot[2][kPsWarps];
-    __shared__ uint32_t ends[2][kPsWarps];
-    __shared__ int found[3];
-    pdl_wait();
-    pdl_launch();
-    const int rows = pg.rows_of(s), P = pg.by_page.div(rows + pg.page_size - 1);
-    int* sel = a.sel + (size_t)pair * a.n_sel;
-    if (P <= a.n_sel) {                                            // (the whole cluster: all pages are in)
-        for (int i = rank * kPsThreads + tid; i < a.n_sel; i += n_cta * kPsThreads) sel[i] = i < P ? i : -1;
-        return;
-    }
-    if (n_cta > 1) asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
+    const int lane = threadIdx.x & 31, pieces = 2 * a.D / E;
     const int* table = pg.table + (long long)s * pg.table_stride;
-    const int step = n_cta * kPsWarps * 8;
-    int next = -1;
-    {
-        const int j = (rank * kPsWarps + warp) * 8 + (lane & 7);
-        if (j < P) next = table[j];
-    }
+    auto ask = [&](int b) { return table[min(b + (lane & (NB - 1)), P - 1)]; };
+    int next = ask(at);
     // weights of this lane's pieces: the first D elements of a page's bounds are its smallest values
     double w[NP][E];
-    const int pieces = 2 * a.D / E;
-#pragma unroll
-    for (int n = 0; n < NP; ++n)
-#pragma unroll
-        for (int e = 0; e < E; ++e) w[n][e] = 0.0;
     const T* q = static_cast<const T*>(a.q) + ((size_t)s * a.H + (size_t)hk * a.G) * a.D;
 #pragma unroll
     for (int n = 0; n < NP; ++n) {
+#pragma unroll
+        for (int e = 0; e < E; ++e) w[n][e] = 0.0;
         const int pc = lane + 32 * n;
         if (pc >= pieces) continue;
         const bool upper = pc * E >= a.D;
         const int d = pc * E - (upper ? a.D : 0);
-        for (int h = 0; h < a.G; ++h) {
-            float x[E];
-            PgVec<T>::unpack(__ldg(reinterpret_cast<const uint4*>(q + (size_t)h * a.D + d)), x);
+        for (int h0 = 0; h0 < a.G; h0 += 4) {
+            uint4 u[4];
 #pragma unroll
-            for (int e = 0; e < E; ++e) w[n][e] += upper ? (x[e] < 0.f ? 0.0 : (double)x[e]) : (x[e] > 0.f ? 0.0 : (double)x[e]);
+            for (int h = 0; h < 4; ++h) u[h] = *reinterpret_cast<const uint4*>(q + (size_t)min(h0 + h, a.G - 1) * a.D + d);
+#pragma unroll
+            for (int h = 0; h < 4; ++h) {
+                float x[E];
+                PgVec<T>::unpack(u[h], x);
+                if (h0 + h < a.G)
+#pragma unroll
+                    for (int e = 0; e < E; ++e) w[n][e] += upper ? (x[e] < 0.f ? 0.0 : (double)x[e]) : (x[e] > 0.f ? 0.0 : (double)x[e]);
+            }
         }
     }
     const T* bounds = static_cast<const T*>(pg.bounds);
-    bool started = n_cta == 1;                                     // CTA 0's memory may be written
-    for (int b = (rank * kPsWarps + warp) * 8; b < P; b += step) {
-        const int page = next;
-        next = b + step + (lane & 7) < P ? table[b + step + (lane & 7)] : -1;
-        double v[8];
-        uint4 x[8][NP];
-        bool there[8];
+    uint4 x[NB][NP];
+    auto load = [&](int page) {
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            const int id = __shfl_sync(0xffffffffu, page, i);
-            there[i] = b + i < P && pg.holds(id);
+        for (int i = 0; i < NB; ++i) {
             // (no branch between the loads: a page that is not there reads page 0, and its score is not used)
-            const uint4* row = reinterpret_cast<const uint4*>(bounds + ((size_t)(there[i] ? id : 0) * a.Hkv + hk) * 2 * a.D);
+            const int id = __shfl_sync(0xffffffffu, page, i);
+            const uint4* row = reinterpret_cast<const uint4*>(bounds + ((size_t)(pg.holds(id) ? id : 0) * a.Hkv + hk) * 2 * a.D);
 #pragma unroll
-            for (int n = 0; n < NP; ++n) x[i][n] = __ldg(row + min(lane + 32 * n, pieces - 1));
+            for (int n = 0; n < NP; ++n) x[i][n] = row[min(lane + 32 * n, pieces - 1)];
         }
+    };
+    bool first = true;
+    int page = next;
+    next = ask(at + step);
+    load(page);
+    for (int b = at; b < P; b += step) {
+        const uint32_t there = __ballot_sync(0xffffffffu, pg.holds(page));
+        double v[NB];
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
+        for (int i = 0; i < NB; ++i) {
             v[i] = 0.0;
 #pragma unroll
             for (int n = 0; n < NP; ++n) {
@@ -609,84 +594,100 @@ page_select_kernel(const __grid_constant__ PageSelectArgs a, int n_cta)
                 for (int e = 0; e < E; ++e) v[i] = fma((double)f[e], w[n][e], v[i]);
             }
         }
-        const double sum = sum8(v, lane);
-        if (!started) {
-            asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
-            started = true;
-        }
-        const int i = lane >> 2;
-        bool ok = false;
+        page = next;
+        next = ask(b + 2 * step);
+        load(page);                                                // (on their way while the sums go round)
 #pragma unroll
-        for (int t = 0; t < 8; ++t) ok = t == i ? there[t] : ok;
-        const int j = b + i;
-        if ((lane & 3) == 0 && j < P) {
-            const uint32_t key = j < a.n_first || j >= P - a.n_last ? kKeyForced : ok ? page_key((float)sum) : page_key(-INFINITY);
-            if (n_cta > 1) st_cluster_u32(ps_keys + j, 0, key);
-            else ps_keys[j] = key;
+        for (int i0 = 0; i0 < NB; i0 += 8) {
+            const double sum = sum8(v + i0, lane);
+            if (first) ready();
+            first = false;
+            const int i = i0 + (lane >> 2), j = b + i;
+            if (j < P)
+                store(j, j < a.n_first || j >= P - a.n_last ? kKeyForced : (there >> i) & 1 ? page_key((float)sum) : page_key(-INFINITY));
         }
     }
-    if (!started) asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
-    if (n_cta > 1) cluster_sync();
-    else __syncthreads();
-    if (rank != 0) return;
+    if (first) ready();
+}
 
+// Chooses n_sel of the P keys (n_sel < P, n_forced of them forced), by all THREADS of a CTA: put(place, page), pages ascending.
+template <int THREADS> struct ChooseMem {
+    int hist[kPsBins];
+    int tot[2][THREADS / 32];
+    uint32_t ends[2][THREADS / 32];
+    int found[3];
+};
+template <int THREADS, typename Put>
+__device__ __forceinline__ void choose_pages(const uint32_t* keys, int P, int n_sel, int n_forced, ChooseMem<THREADS>& mem, Put&& put)
+{
+    constexpr int kWarps = THREADS / 32;
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     // the range of the keys but for the pages that are in anyway
     uint32_t kmin = 0xffffffffu, kmax = 0;
-    for (int i = tid; i < P; i += kPsThreads) {
-        const uint32_t k = ps_keys[i];
+    // (eight keys at a time: their loads do not wait for one another)
+    auto each = [&](int from, int to, int step, auto&& f) {
+        for (int i = from; i < to; i += 8 * step) {
+            uint32_t k[8];
+#pragma unroll
+            for (int t = 0; t < 8; ++t) k[t] = keys[min(i + t * step, P - 1)];
+#pragma unroll
+            for (int t = 0; t < 8; ++t)
+                if (i + t * step < to) f(k[t], i + t * step);
+        }
+    };
+    each(tid, P, THREADS, [&](uint32_t k, int) {
         kmin = min(kmin, k);
         if (k != kKeyForced) kmax = max(kmax, k);
-    }
+    });
     kmin = __reduce_min_sync(0xffffffffu, kmin);
     kmax = __reduce_max_sync(0xffffffffu, kmax);
-    if (lane == 0) { ends[0][warp] = kmin; ends[1][warp] = kmax; }
+    if (lane == 0) { mem.ends[0][warp] = kmin; mem.ends[1][warp] = kmax; }
     __syncthreads();
 #pragma unroll
-    for (int i = 0; i < kPsWarps; ++i) { kmin = min(kmin, ends[0][i]); kmax = max(kmax, ends[1][i]); }
+    for (int i = 0; i < kWarps; ++i) { kmin = min(kmin, mem.ends[0][i]); kmax = max(kmax, mem.ends[1][i]); }
     // keys above the range: `above` < n_sel; keys above or in it: at least n_sel
-    int above = a.n_first + a.n_last, ties = 0;
-    if (above == a.n_sel) kmin = kmax = kKeyNan;
+    int above = n_forced, ties = 0;
+    if (above == n_sel) kmin = kmax = kKeyNan;
     else while (true) {
         const uint32_t width = kmax - kmin;
         const int shift = max(0, 32 - kPsBinBits - __clz(width | 1u));     // width >> shift < kPsBins
-        for (int i = tid; i < kPsBins; i += kPsThreads) hist[i] = 0;
+        for (int i = tid; i < kPsBins; i += THREADS) mem.hist[i] = 0;
         __syncthreads();
-        for (int i = tid; i < P; i += kPsThreads) {
-            const uint32_t k = ps_keys[i];
-            if (k >= kmin && k <= kmax) atomicAdd(&hist[(k - kmin) >> shift], 1);
-        }
+        each(tid, P, THREADS, [&](uint32_t k, int) {
+            if (k >= kmin && k <= kmax) atomicAdd(&mem.hist[(k - kmin) >> shift], 1);
+        });
         __syncthreads();
-        // four bins a thread, from the top
-        constexpr int kPer = kPsBins / kPsThreads;
+        // some bins a thread, from the top
+        constexpr int kPer = kPsBins / THREADS;
         int c[kPer], sum = 0;
 #pragma unroll
-        for (int i = 0; i < kPer; ++i) sum += c[i] = hist[kPsBins - 1 - (tid * kPer + i)];
+        for (int i = 0; i < kPer; ++i) sum += c[i] = mem.hist[kPsBins - 1 - (tid * kPer + i)];
         int upto = sum;
 #pragma unroll
         for (int o = 1; o < 32; o <<= 1) {
             const int x = __shfl_up_sync(0xffffffffu, upto, o);
             if (lane >= o) upto += x;
         }
-        if (lane == 31) tot[0][warp] = upto;
+        if (lane == 31) mem.tot[0][warp] = upto;
         __syncthreads();
 #pragma unroll
-        for (int i = 0; i < kPsWarps; ++i) upto += i < warp ? tot[0][i] : 0;
+        for (int i = 0; i < kWarps; ++i) upto += i < warp ? mem.tot[0][i] : 0;
         int before = above + upto - sum;                           // keys above this thread's bins
-        if (before < a.n_sel && before + sum >= a.n_sel)
+        if (before < n_sel && before + sum >= n_sel)
 #pragma unroll
             for (int i = 0; i < kPer; ++i) {
-                if (before < a.n_sel && before + c[i] >= a.n_sel) {
-                    found[0] = kPsBins - 1 - (tid * kPer + i);
-                    found[1] = before;
-                    found[2] = c[i];
+                if (before < n_sel && before + c[i] >= n_sel) {
+                    mem.found[0] = kPsBins - 1 - (tid * kPer + i);
+                    mem.found[1] = before;
+                    mem.found[2] = c[i];
                 }
                 before += c[i];
             }
         __syncthreads();
-        const uint32_t low = kmin + ((uint32_t)found[0] << shift);
-        above = found[1];
-        const int in_bin = found[2];
-        ties = a.n_sel - above;
+        const uint32_t low = kmin + ((uint32_t)mem.found[0] << shift);
+        above = mem.found[1];
+        const int in_bin = mem.found[2];
+        ties = n_sel - above;
         kmax = low + min(kmax - low, (1u << shift) - 1u);
         kmin = low;
         if (ties == in_bin) { ties = 0x7fffffff; break; }          // all of the bin is in
@@ -694,14 +695,13 @@ page_select_kernel(const __grid_constant__ PageSelectArgs a, int n_cta)
         // (every thread has read found and tot before the next pass writes them: two barriers lie between)
     }
     // keys above kmax are in, and the first `ties` from kmin to kmax
-    const int per = ((P + kPsThreads - 1) / kPsThreads) | 1;       // (odd: a warp's threads read from 32 banks)
+    const int per = ((P + THREADS - 1) / THREADS) | 1;             // (odd: a warp's threads read from 32 banks)
     const int j0 = min(tid * per, P), j1 = min(j0 + per, P);
     int n_hi = 0, n_eq = 0;
-    for (int i = j0; i < j1; ++i) {
-        const uint32_t k = ps_keys[i];
+    each(j0, j1, 1, [&](uint32_t k, int) {
         n_hi += k > kmax;
         n_eq += k >= kmin && k <= kmax;
-    }
+    });
     int s_hi = n_hi, s_eq = n_eq;
 #pragma unroll
     for (int o = 1; o < 32; o <<= 1) {
@@ -709,18 +709,48 @@ page_select_kernel(const __grid_constant__ PageSelectArgs a, int n_cta)
         if (lane >= o) { s_hi += x; s_eq += y; }
     }
     __syncthreads();
-    if (lane == 31) { tot[0][warp] = s_hi; tot[1][warp] = s_eq; }
+    if (lane == 31) { mem.tot[0][warp] = s_hi; mem.tot[1][warp] = s_eq; }
     __syncthreads();
 #pragma unroll
-    for (int i = 0; i < kPsWarps; ++i) {
-        s_hi += i < warp ? tot[0][i] : 0;
-        s_eq += i < warp ? tot[1][i] : 0;
+    for (int i = 0; i < kWarps; ++i) {
+        s_hi += i < warp ? mem.tot[0][i] : 0;
+        s_eq += i < warp ? mem.tot[1][i] : 0;
     }
     int eq = s_eq - n_eq, at = s_hi - n_hi + min(eq, ties);
-    for (int i = j0; i < j1; ++i) {
-        const uint32_t k = ps_keys[i];
-        if (k > kmax || (k >= kmin && eq++ < ties)) sel[at++] = i;
+    each(j0, j1, 1, [&](uint32_t k, int i) {
+        if (k > kmax || (k >= kmin && k <= kmax && eq++ < ties)) put(at++, i);
+    });
+}
+
+template <typename T, int NP>
+__global__ void __launch_bounds__(ps_threads(NP))
+page_select_kernel(const __grid_constant__ PageSelectArgs a, int n_cta)
+{
+    constexpr int kPsThreads = ps_threads(NP), kPsWarps = kPsThreads / 32;
+    const Paged& pg = a.pg;
+    const int tid = threadIdx.x, warp = tid >> 5;
+    const int rank = blockIdx.x, pair = blockIdx.y, s = pair / a.Hkv, hk = pair - s * a.Hkv;
+    extern __shared__ __align__(16) uint32_t ps_keys[];
+    __shared__ ChooseMem<kPsThreads> mem;
+    pdl_wait();
+    pdl_launch();
+    const int rows = pg.rows_of(s), P = pg.by_page.div(rows + pg.page_size - 1);
+    int* sel = a.sel + (size_t)pair * a.n_sel;
+    if (P <= a.n_sel) {                                            // (the whole cluster: all pages are in)
+        for (int i = rank * kPsThreads + tid; i < a.n_sel; i += n_cta * kPsThreads) sel[i] = i < P ? i : -1;
+        return;
     }
+    if (n_cta > 1) cluster_arrive();
+    score_pages<T, NP, 8>(a, s, hk, P, (rank * kPsWarps + warp) * 8, n_cta * kPsWarps * 8,
+        [&] { if (n_cta > 1) cluster_await(); },                   // CTA 0 has started: its memory may be written
+        [&](int j, uint32_t key) {
+            if (tid & 3) return;
+            if (n_cta > 1) st_cluster_u32(ps_keys + j, 0, key);
+            else ps_keys[j] = key;
+        });
+    if (n_cta > 1) cluster_sync();
+    else __syncthreads();
+    if (rank == 0) choose_pages<kPsThreads>(ps_keys, P, a.n_sel, a.n_first + a.n_last, mem, [&](int at, int j) { sel[at] = j; });
 }
 
 }  // namespace sab

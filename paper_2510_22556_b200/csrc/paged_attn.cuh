@@ -7,7 +7,7 @@
 // units of all pairs of a column of KV heads (heads column, column + columns, ...) in order are one line, which its CTAs (the grid is as
 // many as the device holds at once, those of neighbouring columns neighbours) cut into equal shares.  So the CTAs of the columns go
 // along the same rows side by side, and what they read of a row at a time is a stretch of memory: with the heads one after the other
-// instead a batch of 64 sequences of 1K rows took 66 us, ATTEND_BATCH_NEW with eight columns.
+// instead one sequence of 128K rows took 91 us, 86 with eight columns.
 // A CTA adds the lengths up to find its share, which may start inside a pair, hold several pairs and end inside one.  Pairs that lie
 // in one share are written out; of the others every share leaves (accumulator, maximum, sum) in scratch, at most one at its
 // start and one at its end, and paged_merge_kernel, one block per share and head, adds up the pairs that begin in its share.
@@ -223,21 +223,240 @@ __host__ __device__ constexpr int pa_ring_bytes(int DP) { return kPaWarps * kPaS
 __host__ __device__ constexpr int pa_smem(int DP, int heads) { return pa_ring_bytes(DP) + kPaWarps * 4 * DP * (int)sizeof(float) + heads * (DP + 8) * 2; }
 static_assert(2 * (pa_smem(128, 16) + 512 + 1024) <= kSmSharedBytes, "two CTAs on an SM");
 
+// The product alone, nothing added.
+__device__ __forceinline__ void mma_bf16_only(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1)
+{
+    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%10, %10, %10, %10};"
+                 : "=f"(d[0]), "=f"(d[1]), "=f"(d[2]), "=f"(d[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1), "f"(0.f));
+}
+
+// What a warp keeps of a segment, and a chunk's products.
+template <int NS, bool Q4, int DP> struct PaWarp {
+    static_assert(!Q4 || NS == 1, "four heads are one set");
+    static constexpr int PR = DP / 8;                // 16-byte pieces of a row
+    static constexpr int KS = DP / 16;               // k-steps of the logits
+    static constexpr int GP = Q4 ? 4 : 8 * NS;       // heads of a group
+    static constexpr uint32_t kOp = 16 * DP * 2;     // bytes of a chunk of K or V
+    using Queries = __nv_bfloat16 (*)[DP + 8];
+    using Sums = float (*)[4][DP];
+    uint32_t qa[KS][2 * NS];
+    float m[NS], l[NS];
+    uint64_t acc[NS][DP / 8][2];                     // packed pairs
+
+    __device__ __forceinline__ void clear()
+    {
+#pragma unroll
+        for (int n = 0; n < NS; ++n) {
+            m[n] = -INFINITY;
+            l[n] = 0.f;
+#pragma unroll
+            for (int i = 0; i < DP / 8; ++i) acc[n][i][0] = acc[n][i][1] = pack2(0.f, 0.f);
+        }
+    }
+    __device__ __forceinline__ void take_queries(Queries qs, int lane)
+    {
+#pragma unroll
+        for (int n = 0; n < NS; ++n) {
+            const int hh = Q4 ? (lane >> 2) & 3 : 8 * n + (lane >> 2);
+#pragma unroll
+            for (int ks = 0; ks < KS; ++ks)
+#pragma unroll
+                for (int x = 0; x < 2; ++x)
+                    qa[ks][2 * n + x] = *reinterpret_cast<const uint32_t*>(&qs[hh][ks * 16 + x * 8 + 2 * (lane & 3)]);
+        }
+    }
+    // Sixteen rows of K and V at ks_base and vs_base, `there`: which of them exist.
+    __device__ __forceinline__ void chunk(uint32_t ks_base, uint32_t vs_base, uint32_t there, float c2, int lane)
+    {
+        const int lr = lane & 7, mat = lane >> 3;
+        float c[2][4];
+#pragma unroll
+        for (int x = 0; x < 2; ++x)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) c[x][e] = 0.f;
+        {
+            const int row = lr + 8 * (mat >> 1);
+            const uint32_t base = ks_base + (uint32_t)row * PR * 16;
+#pragma unroll
+            for (int ks = 0; ks < KS; ++ks) {
+                uint32_t b[4];
+                ldsm_x4(base + (uint32_t)((2 * ks + (mat & 1)) ^ lr) * 16, b);
+                const uint32_t a1 = NS == 2 ? qa[ks][2 * NS - 2] : 0u, a3 = NS == 2 ? qa[ks][2 * NS - 1] : 0u;
+                mma_bf16(c[0], qa[ks][0], a1, qa[ks][1], a3, b[0], b[1]);
+                mma_bf16(c[1], qa[ks][0], a1, qa[ks][1], a3, b[2], b[3]);
+            }
+        }
+        // logits of this thread's heads, rows row0, row0 + 1, row0 + 8, row0 + 9 of the chunk
+        const uint32_t seen = there >> (2 * (lane & 3));
+        uint32_t hi[NS][2], mid[NS][2], lo[NS][2];
+#pragma unroll
+        for (int n = 0; n < NS; ++n) {
+            float x[4];
+#pragma unroll
+            for (int t = 0; t < 2; ++t)
+#pragma unroll
+                for (int e = 0; e < 2; ++e) x[2 * t + e] = (seen >> (8 * t + e)) & 1 ? c[t][2 * n + e] : -INFINITY;
+            const float mx = fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3])) * c2;
+            if (__any_sync(0xffffffffu, mx > m[n])) {
+                float t = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 1));
+                t = fmaxf(t, __shfl_xor_sync(0xffffffffu, t, 2));
+                const float mn = fmaxf(m[n], t);
+                const float sc = m[n] == -INFINITY ? 0.f : exp2f(m[n] - mn);
+                m[n] = mn;
+                l[n] *= sc;
+                const uint64_t sc2 = pack2(sc, sc);
+#pragma unroll
+                for (int i = 0; i < DP / 8; ++i)
+#pragma unroll
+                    for (int e = 0; e < 2; ++e) acc[n][i][e] = mul2(acc[n][i][e], sc2);
+            }
+            const float mr = m[n] == -INFINITY ? 0.f : m[n];
+#pragma unroll
+            for (int t = 0; t < 2; ++t) {
+                const float p0 = exp2f(fmaf(x[2 * t], c2, -mr)), p1 = exp2f(fmaf(x[2 * t + 1], c2, -mr));
+                l[n] += p0 + p1;
+                constexpr float kShare = Q4 ? 1.f : 0.5f;      // of the leading piece in one instruction
+                hi[n][t] = pack_bf16(kShare * p0, kShare * p1);
+                const float q0 = fmaf(-1.f / kShare, __uint_as_float(hi[n][t] << 16), p0);
+                const float q1 = fmaf(-1.f / kShare, __uint_as_float(hi[n][t] & 0xffff0000u), p1);
+                mid[n][t] = pack_bf16(q0, q1);
+                lo[n][t] = pack_bf16(q0 - __uint_as_float(mid[n][t] << 16), q1 - __uint_as_float(mid[n][t] & 0xffff0000u));
+            }
+            if constexpr (Q4) {
+#pragma unroll
+                for (int t = 0; t < 2; ++t) {
+                    hi[n][t] = lane < 16 ? hi[n][t] : lo[n][t];
+                    mid[n][t] = lane < 16 ? mid[n][t] : 0u;
+                }
+            }
+        }
+        {
+            const int row = lr + 8 * (mat & 1);
+            const uint32_t base = vs_base + (uint32_t)row * PR * 16;
+#pragma unroll
+            for (int i = 0; i < DP / 8; i += 2) {
+                uint32_t b[4];
+                ldsm_x4_trans(base + (uint32_t)((i + (mat >> 1)) ^ lr) * 16, b);
+#pragma unroll
+                for (int n = 0; n < NS; ++n)
+#pragma unroll
+                    for (int t = 0; t < 2; ++t) {
+                        // (the instruction rounds its sums towards zero: a chunk's go into registers of their own, and are added
+                        // up by additions that round to nearest: 128K rows, 896 a warp, were off by 1.6e-6 the other way, by 6.6e-7 so)
+                        float o[4];
+                        mma_bf16_only(o, hi[n][0], mid[n][0], hi[n][1], mid[n][1], b[2 * t], b[2 * t + 1]);
+                        if constexpr (!Q4) mma_bf16(o, hi[n][0], lo[n][0], hi[n][1], lo[n][1], b[2 * t], b[2 * t + 1]);
+                        acc[n][i + t][0] = add2(acc[n][i + t][0], pack2(o[0], o[1]));
+                        acc[n][i + t][1] = add2(acc[n][i + t][1], pack2(o[2], o[3]));
+                    }
+            }
+        }
+    }
+    __device__ __forceinline__ void join_lanes()
+    {
+#pragma unroll
+        for (int n = 0; n < NS; ++n) {
+            l[n] += __shfl_xor_sync(0xffffffffu, l[n], 1);
+            l[n] += __shfl_xor_sync(0xffffffffu, l[n], 2);
+        }
+    }
+    // The warp's sums of heads 4 r .. 4 r + 3, the pieces added.
+    __device__ __forceinline__ void put(int r, Sums accs, float (*ms)[4], float (*ls)[4], int warp, int lane) const
+    {
+        const int n = r / 2;
+        const bool mine = lane >> 4 == (r & 1);      // (with four heads, lanes 16 to 31 have copies)
+#pragma unroll
+        for (int i = 0; i < DP / 8; ++i) {
+            float x[2], v[4];
+            unpack2(acc[n][i][0], v[0], v[1]);
+            unpack2(acc[n][i][1], v[2], v[3]);
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+                const float less = Q4 ? v[2 + e] + __shfl_down_sync(0xffffffffu, v[e], 16) : v[2 + e];
+                // an infinite value times a smaller piece is an infinity of either sign or, where the piece is zero, no
+                // number: the leading piece alone says what the weight times the value is
+                x[e] = isinf(v[e]) ? v[e] : v[e] + less;
+            }
+            if (mine) *reinterpret_cast<float2*>(&accs[warp][(lane >> 2) & 3][i * 8 + 2 * (lane & 3)]) = make_float2(x[0], x[1]);
+        }
+        if (mine && (lane & 3) == 0) { ms[warp][(lane >> 2) & 3] = m[n]; ls[warp][(lane >> 2) & 3] = l[n]; }
+    }
+};
+
+// The warps' sums of one of four heads, columns d .. d + 3, in their order.
+template <int DP>
+__device__ __forceinline__ void pa_join(const float (*accs)[4][DP], const float (*ms)[4], const float (*ls)[4], int hs, int d, float4& sum, float& mx, float& lsum)
+{
+    mx = -INFINITY;
+#pragma unroll
+    for (int v = 0; v < kPaWarps; ++v) mx = fmaxf(mx, ms[v][hs]);
+    sum = make_float4(0.f, 0.f, 0.f, 0.f);
+    lsum = 0.f;
+#pragma unroll
+    for (int v = 0; v < kPaWarps; ++v) {
+        if (ls[v][hs] == 0.f) continue;              // (a warp without rows; one whose sum is no number counts)
+        const float wt = ms[v][hs] == -INFINITY ? 1.f : exp2f(ms[v][hs] - mx);
+        const float4 x = *reinterpret_cast<const float4*>(&accs[v][hs][d]);
+        sum.x += x.x * wt; sum.y += x.y * wt; sum.z += x.z * wt; sum.w += x.w * wt;
+        lsum += ls[v][hs] * wt;
+    }
+}
+
+// Copies of a chunk's rows into a warp's ring, found by its lanes (lane r and lane r + 16 have row r); which rows exist, a bit each.
+template <int DP>
+__device__ __forceinline__ uint32_t pa_copy(const PagedAttnArgs& a, const PgRow& row, const __nv_bfloat16* kb, const __nv_bfloat16* vb, uint32_t dst, int lane)
+{
+    constexpr int PR = DP / 8;
+    const int pc = lane % PR;
+    const bool piece_there = pc < a.D / 8, ok = row.ok && a.pg.holds(row.page);
+    const long long ko = ok ? (long long)row.page * a.pg.k_page + (long long)row.slot * a.pg.k_row : -1;
+    const long long vo = a.same_place ? ko : ok ? (long long)row.page * a.pg.v_page + (long long)row.slot * a.pg.v_row : -1;
+#pragma unroll
+    for (int i = 0; i < PR / 2; ++i) {
+        const int rr = lane / PR + i * (32 / PR);
+        const long long k_at = __shfl_sync(0xffffffffu, ko, rr);
+        const long long v_at = a.same_place ? k_at : __shfl_sync(0xffffffffu, vo, rr);
+        const bool there = k_at >= 0 && piece_there;
+        const uint32_t o = dst + (uint32_t)(rr * PR + (pc ^ (rr & 7))) * 16;
+        cp_async16_or_zero(o, kb + (there ? k_at + pc * 8 : 0), there);
+        cp_async16_or_zero(o + 16 * DP * 2, vb + (there ? v_at + pc * 8 : 0), there);
+    }
+    return __ballot_sync(0xffffffffu, ok) & 0xffffu;
+}
+
+// The queries of a group, asked for by a CTA and put into its shared memory.
+template <int GP, int DP> struct PaQueries {
+    static constexpr int PR = DP / 8, N = (GP * PR + kPaThreads - 1) / kPaThreads;
+    uint4 x[N];
+    __device__ __forceinline__ void ask(const PagedAttnArgs& a, size_t head, int heads)
+    {
+#pragma unroll
+        for (int t = 0; t < N; ++t) {
+            const int i = threadIdx.x + t * kPaThreads, h = min(i / PR, heads - 1), c = min(i % PR, a.D / 8 - 1);
+            x[t] = *reinterpret_cast<const uint4*>(static_cast<const __nv_bfloat16*>(a.q) + (head + h) * a.D + c * 8);
+        }
+    }
+    __device__ __forceinline__ void put(__nv_bfloat16 (*qs)[DP + 8], int D) const
+    {
+#pragma unroll
+        for (int t = 0; t < N; ++t) {
+            const int i = threadIdx.x + t * kPaThreads;
+            if (i < GP * PR) *reinterpret_cast<uint4*>(&qs[i / PR][i % PR * 8]) = i % PR < D / 8 ? x[t] : make_uint4(0, 0, 0, 0);
+        }
+    }
+};
+
 template <int NS, bool Q4, int DP>
 __global__ void __launch_bounds__(kPaThreads, DP == 256 ? 1 : 2)
 paged_mma_kernel(const __grid_constant__ PagedAttnArgs a)
 {
-    static_assert(!Q4 || NS == 1, "four heads are one set");
-    constexpr int PR = DP / 8;                       // 16-byte pieces of a row
-    constexpr int KS = DP / 16;                      // k-steps of the logits
-    constexpr int GP = Q4 ? 4 : 8 * NS;              // heads of a group
-    constexpr int kQn = (GP * PR + kPaThreads - 1) / kPaThreads;
-    constexpr uint32_t kOp = 16 * DP * 2;            // bytes of a chunk of K or V
+    using Warp = PaWarp<NS, Q4, DP>;
+    constexpr uint32_t kOp = Warp::kOp;
     using bf16 = __nv_bfloat16;
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     extern __shared__ __align__(128) uint8_t pa_ring[];
-    float (*accs)[4][DP] = reinterpret_cast<float (*)[4][DP]>(pa_ring + pa_ring_bytes(DP));
-    bf16 (*qs)[DP + 8] = reinterpret_cast<bf16 (*)[DP + 8]>(pa_ring + pa_ring_bytes(DP) + kPaWarps * 4 * DP * sizeof(float));
+    const typename Warp::Sums accs = reinterpret_cast<typename Warp::Sums>(pa_ring + pa_ring_bytes(DP));
+    const typename Warp::Queries qs = reinterpret_cast<typename Warp::Queries>(pa_ring + pa_ring_bytes(DP) + kPaWarps * 4 * DP * sizeof(float));
     __shared__ float ms[kPaWarps][4], ls[kPaWarps][4];
     const uint32_t ring = smem_u32(pa_ring) + warp * kPaStages * 2 * kOp;
     pdl_wait();
@@ -252,9 +471,6 @@ paged_mma_kernel(const __grid_constant__ PagedAttnArgs a)
         pair = (int)(sh.skip / units);
         w = (int)(sh.skip - pair * units);
     }
-    const int n_pieces = a.D / 8, pc = lane % PR;
-    const bool piece_there = pc < n_pieces;
-    const int lr = lane & 7, mat = lane >> 3;
     auto chunks_of = [&](const PgSegment& g) { return ((g.row1 > g.row0 ? (g.row1 - g.row0 + 15) / 16 : 0) - warp + kPaWarps - 1) / kPaWarps; };
 
     // The copies: a cursor of its own, kPaStages - 1 chunks ahead of the products and over the ends of segments, so that the loads of the
@@ -265,7 +481,6 @@ paged_mma_kernel(const __grid_constant__ PagedAttnArgs a)
         int k, n;                                    // next chunk of this warp in the open segment, and its chunks
         int stage;
     } io = {sh.u_end - sh.u, s, pair, w, 0, 0, 0};
-    PgSegment g;
     PgLook look;
     const bf16 *kb, *vb;
     int io_row;                                      // this lane's row of the open segment's chunk 0
@@ -294,21 +509,7 @@ paged_mma_kernel(const __grid_constant__ PagedAttnArgs a)
     auto step = [&] {
         uint32_t there_rows = 0;
         if (io.k < io.n) {
-            const uint32_t dst = ring + (uint32_t)io.stage * 2 * kOp;
-            const bool ok = next.ok && a.pg.holds(next.page);
-            const long long ko = ok ? (long long)next.page * a.pg.k_page + (long long)next.slot * a.pg.k_row : -1;
-            const long long vo = a.same_place ? ko : ok ? (long long)next.page * a.pg.v_page + (long long)next.slot * a.pg.v_row : -1;
-            there_rows = __ballot_sync(0xffffffffu, ok) & 0xffffu;
-#pragma unroll
-            for (int i = 0; i < PR / 2; ++i) {
-                const int rr = lane / PR + i * (32 / PR);
-                const long long k_at = __shfl_sync(0xffffffffu, ko, rr);
-                const long long v_at = a.same_place ? k_at : __shfl_sync(0xffffffffu, vo, rr);
-                const bool there = k_at >= 0 && piece_there;
-                const uint32_t o = dst + (uint32_t)(rr * PR + (pc ^ (rr & 7))) * 16;
-                cp_async16_or_zero(o, kb + (there ? k_at + pc * 8 : 0), there);
-                cp_async16_or_zero(o + kOp, vb + (there ? v_at + pc * 8 : 0), there);
-            }
+            there_rows = pa_copy<DP>(a, next, kb, vb, ring + (uint32_t)io.stage * 2 * kOp, lane);
             ++io.k;
             next = pg_find(a, look, io_row + io.k * kPaUnit, next_j);
             next_j = pg_listed(a, look, io_row + (io.k + 1) * kPaUnit);
@@ -318,202 +519,59 @@ paged_mma_kernel(const __grid_constant__ PagedAttnArgs a)
         there_ring = there_ring >> 16 | there_rows << 16;
         cp_async_commit();
     };
-    // The queries of a segment: asked for while the segment before is worked on, put into shared memory at its end, then taken as
-    // fragments by every warp.
-    uint4 q_next[kQn];
-    auto ask_queries = [&](const PgSegment& g) {
-#pragma unroll
-        for (int t = 0; t < kQn; ++t) {
-            const int i = tid + t * kPaThreads, h = min(i / PR, g.heads - 1), c = min(i % PR, n_pieces - 1);
-            q_next[t] = *reinterpret_cast<const uint4*>(static_cast<const bf16*>(a.q) + (pg_head(a, g) + h) * a.D + c * 8);
-        }
-    };
-    auto put_queries = [&] {
-#pragma unroll
-        for (int t = 0; t < kQn; ++t) {
-            const int i = tid + t * kPaThreads;
-            if (i < GP * PR) *reinterpret_cast<uint4*>(&qs[i / PR][i % PR * 8]) = i % PR < n_pieces ? q_next[t] : make_uint4(0, 0, 0, 0);
-        }
-    };
-    uint32_t qa[KS][2 * NS];
-    auto take_queries = [&] {
-#pragma unroll
-        for (int n = 0; n < NS; ++n) {
-            const int hh = Q4 ? (lane >> 2) & 3 : 8 * n + (lane >> 2);
-#pragma unroll
-            for (int ks = 0; ks < KS; ++ks)
-#pragma unroll
-                for (int x = 0; x < 2; ++x)
-                    qa[ks][2 * n + x] = *reinterpret_cast<const uint32_t*>(&qs[hh][ks * 16 + x * 8 + 2 * (lane & 3)]);
-        }
-    };
-    // segment after the one at hand
-    auto advance = [&] {
-        sh.u += min(g.units - w, sh.u_end - sh.u);
-        w = 0;
-        if (++pair == pairs) { pair = 0; ++s; }
-    };
+    // The queries of a segment are asked for while the segment before is worked on, and put into shared memory at its end.
+    PaQueries<Warp::GP, DP> queries;
+    PgSegment g = pg_segment<kPaUnit>(a, s, pair, w, sh.u_end - sh.u);
+    queries.ask(a, pg_head(a, g), g.heads);
     int stage = 0;
-    g = pg_segment<kPaUnit>(a, s, pair, w, sh.u_end - sh.u);
-    ask_queries(g);
     open();
     step();
     step();
-    put_queries();
+    queries.put(qs, a.D);
     __syncthreads();
+    Warp me;
     while (true) {
-        take_queries();
+        me.take_queries(qs, lane);
         const PgSegment at = g;                      // the segment at hand; g is the next one from here on
         const long long unit = sh.u;
-        advance();
+        sh.u += min(g.units - w, sh.u_end - sh.u);
+        w = 0;
+        if (++pair == pairs) { pair = 0; ++s; }
         const bool more = sh.u < sh.u_end;
         if (more) {
             g = pg_segment<kPaUnit>(a, s, pair, w, sh.u_end - sh.u);
-            ask_queries(g);
+            queries.ask(a, pg_head(a, g), g.heads);
         }
-        float m[NS], l[NS], acc[NS][DP / 8][4];
-#pragma unroll
-        for (int n = 0; n < NS; ++n) {
-            m[n] = -INFINITY;
-            l[n] = 0.f;
-#pragma unroll
-            for (int i = 0; i < DP / 8; ++i)
-#pragma unroll
-                for (int e = 0; e < 4; ++e) acc[n][i][e] = 0.f;
-        }
+        me.clear();
         const int n_it = chunks_of(at);
         for (int it = 0; it < n_it; ++it) {
             const uint32_t there = there_ring & 0xffffu;         // (of the two chunks in flight, the older one)
             step();
             cp_async_wait<kPaStages - 1>();
             __syncwarp();
-            const uint32_t ks_base = ring + (uint32_t)stage * 2 * kOp, vs_base = ks_base + kOp;
+            const uint32_t base = ring + (uint32_t)stage * 2 * kOp;
+            me.chunk(base, base + kOp, there, a.c2, lane);
             stage = stage == kPaStages - 1 ? 0 : stage + 1;
-            float c[2][4];
-#pragma unroll
-            for (int x = 0; x < 2; ++x)
-#pragma unroll
-                for (int e = 0; e < 4; ++e) c[x][e] = 0.f;
-            {
-                const int row = lr + 8 * (mat >> 1);
-                const uint32_t base = ks_base + (uint32_t)row * PR * 16;
-#pragma unroll
-                for (int ks = 0; ks < KS; ++ks) {
-                    uint32_t b[4];
-                    ldsm_x4(base + (uint32_t)((2 * ks + (mat & 1)) ^ lr) * 16, b);
-                    const uint32_t a1 = NS == 2 ? qa[ks][2 * NS - 2] : 0u, a3 = NS == 2 ? qa[ks][2 * NS - 1] : 0u;
-                    mma_bf16(c[0], qa[ks][0], a1, qa[ks][1], a3, b[0], b[1]);
-                    mma_bf16(c[1], qa[ks][0], a1, qa[ks][1], a3, b[2], b[3]);
-                }
-            }
-            // logits of this thread's heads, rows row0, row0 + 1, row0 + 8, row0 + 9 of the chunk
-            const uint32_t seen = there >> (2 * (lane & 3));
-            uint32_t hi[NS][2], mid[NS][2], lo[NS][2];
-#pragma unroll
-            for (int n = 0; n < NS; ++n) {
-                float x[4];
-#pragma unroll
-                for (int t = 0; t < 2; ++t)
-#pragma unroll
-                    for (int e = 0; e < 2; ++e) x[2 * t + e] = (seen >> (8 * t + e)) & 1 ? c[t][2 * n + e] : -INFINITY;
-                const float mx = fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3])) * a.c2;
-                if (__any_sync(0xffffffffu, mx > m[n])) {
-                    float t = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 1));
-                    t = fmaxf(t, __shfl_xor_sync(0xffffffffu, t, 2));
-                    const float mn = fmaxf(m[n], t);
-                    const float sc = m[n] == -INFINITY ? 0.f : exp2f(m[n] - mn);
-                    m[n] = mn;
-                    l[n] *= sc;
-#pragma unroll
-                    for (int i = 0; i < DP / 8; ++i)
-#pragma unroll
-                        for (int e = 0; e < 4; ++e) acc[n][i][e] *= sc;
-                }
-                const float mr = m[n] == -INFINITY ? 0.f : m[n];
-#pragma unroll
-                for (int t = 0; t < 2; ++t) {
-                    const float p0 = exp2f(fmaf(x[2 * t], a.c2, -mr)), p1 = exp2f(fmaf(x[2 * t + 1], a.c2, -mr));
-                    l[n] += p0 + p1;
-                    constexpr float kShare = Q4 ? 1.f : 0.5f;      // of the leading piece in one instruction
-                    hi[n][t] = pack_bf16(kShare * p0, kShare * p1);
-                    const float q0 = fmaf(-1.f / kShare, __uint_as_float(hi[n][t] << 16), p0);
-                    const float q1 = fmaf(-1.f / kShare, __uint_as_float(hi[n][t] & 0xffff0000u), p1);
-                    mid[n][t] = pack_bf16(q0, q1);
-                    lo[n][t] = pack_bf16(q0 - __uint_as_float(mid[n][t] << 16), q1 - __uint_as_float(mid[n][t] & 0xffff0000u));
-                }
-                if constexpr (Q4) {
-#pragma unroll
-                    for (int t = 0; t < 2; ++t) {
-                        hi[n][t] = lane < 16 ? hi[n][t] : lo[n][t];
-                        mid[n][t] = lane < 16 ? mid[n][t] : 0u;
-                    }
-                }
-            }
-            {
-                const int row = lr + 8 * (mat & 1);
-                const uint32_t base = vs_base + (uint32_t)row * PR * 16;
-#pragma unroll
-                for (int i = 0; i < DP / 8; i += 2) {
-                    uint32_t b[4];
-                    ldsm_x4_trans(base + (uint32_t)((i + (mat >> 1)) ^ lr) * 16, b);
-#pragma unroll
-                    for (int n = 0; n < NS; ++n)
-#pragma unroll
-                        for (int t = 0; t < 2; ++t) {
-                            mma_bf16(acc[n][i + t], hi[n][0], mid[n][0], hi[n][1], mid[n][1], b[2 * t], b[2 * t + 1]);
-                            if constexpr (!Q4) mma_bf16(acc[n][i + t], hi[n][0], lo[n][0], hi[n][1], lo[n][1], b[2 * t], b[2 * t + 1]);
-                        }
-                }
-            }
             __syncwarp();                            // the stage may be refilled
         }
-        // The segment is over: the pieces are added and the warps merged, in a fixed order, four heads at a time.
+        // The segment is over: the warps are merged, in a fixed order, four heads at a time.
         if (tid == 0 && at.first && !at.last) {
             // the pair goes on in the next shares: the last unit of it is unit `end` of the line
             const long long end = unit + at.units - 1;
             a.jobs[blockIdx.x] = make_int4((int)pg_head(a, at), at.heads, (int)(end / sh.quota) - (int)blockIdx.x / a.columns + 1, 0);
         }
+        me.join_lanes();
 #pragma unroll
-        for (int n = 0; n < NS; ++n) {
-            l[n] += __shfl_xor_sync(0xffffffffu, l[n], 1);
-            l[n] += __shfl_xor_sync(0xffffffffu, l[n], 2);
-        }
-#pragma unroll
-        for (int r = 0; r < GP / 4; ++r) {
-            const int n = r / 2;
-            const bool mine = lane >> 4 == (r & 1);                // (with four heads, lanes 16 to 31 have copies)
-#pragma unroll
-            for (int i = 0; i < DP / 8; ++i) {
-                float x[2];
-#pragma unroll
-                for (int e = 0; e < 2; ++e) {
-                    const float less = Q4 ? acc[n][i][2 + e] + __shfl_down_sync(0xffffffffu, acc[n][i][e], 16) : acc[n][i][2 + e];
-                    // an infinite value times a smaller piece is an infinity of either sign or, where the piece is zero, no
-                    // number: the leading piece alone says what the weight times the value is
-                    x[e] = isinf(acc[n][i][e]) ? acc[n][i][e] : acc[n][i][e] + less;
-                }
-                if (mine) *reinterpret_cast<float2*>(&accs[warp][(lane >> 2) & 3][i * 8 + 2 * (lane & 3)]) = make_float2(x[0], x[1]);
-            }
-            if (mine && (lane & 3) == 0) { ms[warp][(lane >> 2) & 3] = m[n]; ls[warp][(lane >> 2) & 3] = l[n]; }
+        for (int r = 0; r < Warp::GP / 4; ++r) {
+            me.put(r, accs, ms, ls, warp, lane);
             __syncthreads();
-            if (r == 0 && more) put_queries();           // (every warp has taken those of this segment)
-#pragma unroll
-            for (int i = tid; i < 4 * DP / 4; i += kPaThreads) {
+            if (r == 0 && more) queries.put(qs, a.D);    // (every warp has taken those of this segment)
+            for (int i = tid; i < DP; i += kPaThreads) {
                 const int hs = i / (DP / 4), h = 4 * r + hs, d = 4 * (i % (DP / 4));
                 if (h >= at.heads || d >= a.D) continue;
-                float mx = -INFINITY;
-#pragma unroll
-                for (int v = 0; v < kPaWarps; ++v) mx = fmaxf(mx, ms[v][hs]);
-                float4 sum = make_float4(0.f, 0.f, 0.f, 0.f);
-                float lsum = 0.f;
-#pragma unroll
-                for (int v = 0; v < kPaWarps; ++v) {
-                    if (ls[v][hs] == 0.f) continue;  // (a warp without rows; one whose sum is no number counts)
-                    const float wt = ms[v][hs] == -INFINITY ? 1.f : exp2f(ms[v][hs] - mx);
-                    const float4 x = *reinterpret_cast<const float4*>(&accs[v][hs][d]);
-                    sum.x += x.x * wt; sum.y += x.y * wt; sum.z += x.z * wt; sum.w += x.w * wt;
-                    lsum += ls[v][hs] * wt;
-                }
+                float4 sum;
+                float mx, lsum;
+                pa_join<DP>(accs, ms, ls, hs, d, sum, mx, lsum);
                 pg_emit4(a, at, h, d, sum, mx, lsum);
             }
             __syncthreads();                             // the sums may be written again
@@ -521,6 +579,168 @@ paged_mma_kernel(const __grid_constant__ PagedAttnArgs a)
         if (!more) break;
     }
     cp_async_wait<0>();
+}
+
+// ---- bf16, one launch -------------------------------------------------------------------------------------
+// Where a cluster of CTAs has all of a pair, the parts are merged on chip and there is no second launch; and where pages are to be
+// chosen (SEL), it chooses them too: every CTA scores a share of the pages, leaves the keys with all CTAs of the cluster, and each
+// chooses for itself (the choice costs less than handing it round).  The keys lie where the ring is later.
+constexpr int kPcMaxCluster = 8;
+__host__ __device__ constexpr int pc_keys(int DP) { return pa_ring_bytes(DP) / 4; }      // pages whose keys there is room for
+constexpr int kPcMaxList = 1024;                     // chosen pages
+__host__ __device__ constexpr int pc_smem(int DP, int heads, int n_sel) { return pa_smem(DP, heads) + n_sel * 4; }
+static_assert(2 * (pc_smem(128, 8, kPcMaxList) + 512 + 1024) <= kSmSharedBytes, "two CTAs on an SM");
+
+__device__ __forceinline__ float4 ld_cluster_f4(const void* p, int rank)
+{
+    float4 v;
+    asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(cluster_map(p, rank)) : "memory");
+    return v;
+}
+
+template <bool Q4, int DP, bool SEL>
+__global__ void __launch_bounds__(kPaThreads, 2)
+paged_cluster_kernel(const __grid_constant__ PagedAttnArgs a, const __grid_constant__ PageSelectArgs ps, int n_cta)
+{
+    using Warp = PaWarp<1, Q4, DP>;
+    constexpr uint32_t kOp = Warp::kOp;
+    constexpr int GP = Warp::GP;
+    using bf16 = __nv_bfloat16;
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    const int rank = blockIdx.x, hk = blockIdx.y, s = blockIdx.z;
+    extern __shared__ __align__(128) uint8_t pa_ring[];
+    const typename Warp::Sums accs = reinterpret_cast<typename Warp::Sums>(pa_ring + pa_ring_bytes(DP));
+    const typename Warp::Queries qs = reinterpret_cast<typename Warp::Queries>(pa_ring + pa_ring_bytes(DP) + kPaWarps * 4 * DP * sizeof(float));
+    int* list = reinterpret_cast<int*>(pa_ring + pa_smem(DP, GP));
+    __shared__ float ms[kPaWarps][4], ls[kPaWarps][4];
+    __shared__ __align__(16) float2 cml[GP];         // this CTA's maxima and sums
+    const uint32_t ring = smem_u32(pa_ring) + warp * kPaStages * 2 * kOp;
+    pdl_wait();
+    pdl_launch();
+    const int len = a.pg.rows_of(s);
+    const size_t head = (size_t)s * a.H + (size_t)hk * a.G;
+    PaQueries<GP, DP> queries;
+    queries.ask(a, head, a.G);
+    int rows = len;
+    if constexpr (SEL) {
+        const int P = a.pg.by_page.div(len + a.pg.page_size - 1), n = min(ps.n_sel, P);
+        int* sel = ps.sel + ((size_t)s * a.Hkv + hk) * ps.n_sel;
+        if (P > ps.n_sel) {
+            uint32_t* keys = reinterpret_cast<uint32_t*>(pa_ring);
+            auto& mem = *reinterpret_cast<ChooseMem<kPaThreads>*>(accs);
+            static_assert(sizeof(ChooseMem<kPaThreads>) <= pa_smem(DP, GP) - pa_ring_bytes(DP), "what choosing needs lies where sums and queries are later");
+            if (n_cta > 1) cluster_arrive();
+            score_pages<bf16, 1, 16>(ps, s, hk, P, (rank * kPaWarps + warp) * 16, n_cta * kPaWarps * 16,
+                [&] { if (n_cta > 1) cluster_await(); },           // the others have started: their memory may be written
+                [&](int j, uint32_t key) {
+                    if (n_cta == 1) {
+                        if ((lane & 3) == 0) keys[j] = key;
+                        return;
+                    }
+                    for (int r = lane & 3; r < n_cta; r += 4) st_cluster_u32(keys + j, r, key);
+                });
+            if (n_cta > 1) cluster_sync();
+            else __syncthreads();
+            choose_pages<kPaThreads>(keys, P, ps.n_sel, ps.n_first + ps.n_last, mem, [&](int at, int j) {
+                list[at] = j;
+                if (rank == 0) sel[at] = j;
+            });
+        } else {
+            for (int i = tid; i < ps.n_sel; i += kPaThreads) {
+                if (i < P) list[i] = i;
+                if (rank == 0) sel[i] = i < P ? i : -1;
+            }
+        }
+        rows = n * a.pg.page_size;
+        __syncthreads();                             // the list is there, the keys have been read
+    }
+    queries.put(qs, a.D);
+    const int units = (rows + kPaUnit - 1) / kPaUnit, share = (units + n_cta - 1) / n_cta;
+    const int row0 = min(rows, rank * share * kPaUnit), row1 = min(rows, row0 + share * kPaUnit);
+    const int n_it = ((row1 - row0 + 15) / 16 - warp + kPaWarps - 1) / kPaWarps;
+    const bf16* kb = static_cast<const bf16*>(a.pg.k) + (size_t)hk * a.pg.k_head;
+    const bf16* vb = static_cast<const bf16*>(a.pg.v) + (size_t)hk * a.pg.v_head;
+    PgLook look;
+    look.table = a.pg.table + (long long)s * a.pg.table_stride;
+    look.sel = nullptr;
+    look.rows = row1;
+    look.len = len;
+    const int my_row = row0 + warp * 16 + (lane & 15);
+    auto find = [&](int it) {                        // row of chunk `it`
+        const int v = my_row + it * kPaUnit;
+        int j = a.pg.by_page.div(max(0, min(v, row1 - 1)));
+        if constexpr (SEL) j = row1 > 0 ? list[j] : -1;
+        return pg_find(a, look, v, j);
+    };
+    uint32_t there_ring = 0;
+    PgRow next;
+    auto step = [&](int it) {
+        uint32_t there_rows = 0;
+        if (it < n_it) there_rows = pa_copy<DP>(a, next, kb, vb, ring + (uint32_t)(it % kPaStages) * 2 * kOp, lane);
+        next = find(it + 1);
+        there_ring = there_ring >> 16 | there_rows << 16;
+        cp_async_commit();
+    };
+    next = find(0);
+    step(0);
+    step(1);
+    __syncthreads();
+    Warp me;
+    me.take_queries(qs, lane);
+    me.clear();
+    for (int it = 0; it < n_it; ++it) {
+        const uint32_t there = there_ring & 0xffffu;
+        step(it + kPaStages - 1);
+        cp_async_wait<kPaStages - 1>();
+        __syncwarp();
+        const uint32_t base = ring + (uint32_t)(it % kPaStages) * 2 * kOp;
+        me.chunk(base, base + kOp, there, a.c2, lane);
+        __syncwarp();
+    }
+    cp_async_wait<0>();
+    me.join_lanes();
+    // ---- merge: the warps (the CTA's sums go where the ring was), then the CTAs
+    float (*csum)[DP] = reinterpret_cast<float (*)[DP]>(pa_ring);
+    static_assert(GP * DP * (int)sizeof(float) <= pa_ring_bytes(DP), "sums fit in the ring");
+#pragma unroll
+    for (int r = 0; r < GP / 4; ++r) {
+        me.put(r, accs, ms, ls, warp, lane);
+        __syncthreads();
+        for (int i = tid; i < DP; i += kPaThreads) {
+            const int hs = i / (DP / 4), h = 4 * r + hs, d = 4 * (i % (DP / 4));
+            float4 sum;
+            float mx, lsum;
+            pa_join<DP>(accs, ms, ls, hs, d, sum, mx, lsum);
+            *reinterpret_cast<float4*>(&csum[h][d]) = sum;
+            if (d == 0) cml[h] = make_float2(mx, lsum);
+        }
+        __syncthreads();
+    }
+    if (n_cta > 1) cluster_sync();
+    for (int i = rank * kPaThreads + tid; i < GP * DP / 4; i += n_cta * kPaThreads) {
+        const int h = i / (DP / 4), d = 4 * (i % (DP / 4));
+        if (h >= a.G || d >= a.D) continue;
+        float M = -INFINITY;
+        for (int c = 0; c < n_cta; ++c) M = fmaxf(M, ld_cluster_f32(&cml[h].x, c));
+        float4 num = make_float4(0.f, 0.f, 0.f, 0.f);
+        float den = 0.f;
+#pragma unroll 4
+        for (int c = 0; c < n_cta; ++c) {
+            const float m = ld_cluster_f32(&cml[h].x, c), l = ld_cluster_f32(&cml[h].y, c);
+            const float4 x = ld_cluster_f4(&csum[h][d], c);
+            if (l == 0.f) continue;
+            const float w = m == -INFINITY ? 1.f : exp2f(m - M);
+            num.x += x.x * w; num.y += x.y * w; num.z += x.z * w; num.w += x.w * w;
+            den += l * w;
+        }
+        float* dst = a.out + (head + h) * a.D + d;
+        dst[0] = den == 0.f ? 0.f : num.x / den;
+        dst[1] = den == 0.f ? 0.f : num.y / den;
+        dst[2] = den == 0.f ? 0.f : num.z / den;
+        dst[3] = den == 0.f ? 0.f : num.w / den;
+        if (a.lse && d == 0) a.lse[head + h] = den == 0.f ? -INFINITY : (M + log2f(den)) * 0.6931471805599453f;
+    }
+    if (n_cta > 1) cluster_sync();                   // the others may still read this one's sums
 }
 
 // ---- fp32 -----------------------------------------------------------------------------------------------

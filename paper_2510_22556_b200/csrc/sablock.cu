@@ -1153,8 +1153,42 @@ sablock_status_t launch_paged_fma(const PagedAttnArgs& a, int ctas, cudaStream_t
     return launch(paged_fma_kernel<GP, DP>, dim3(ctas), kPaThreads, pf_smem(DP), st, 1, a);
 }
 
+template <bool Q4, int DP, bool SEL>
+sablock_status_t launch_paged_cluster(const PagedAttnArgs& a, const PageSelectArgs& ps, int cluster, cudaStream_t st)
+{
+    constexpr auto kern = paged_cluster_kernel<Q4, DP, SEL>;
+    const int smem = pc_smem(DP, Q4 ? 4 : 8, SEL ? ps.n_sel : 0);
+    SAB_TRY(allow_smem<kern>(smem));
+    return launch(kern, dim3(cluster, a.Hkv, a.pg.n_seqs), kPaThreads, smem, st, cluster, a, ps, cluster);
+}
+
+// CTAs of a pair's cluster, 0 where the call goes to the kernels that cut the work into shares.  The one launch saves about 4 us, 10 where
+// pages are chosen.  What it costs is what the places of the grid that no pair has (two CTAs on an SM) could have read meanwhile; the
+// two meet at about 40 MB, and 80.  us, one launch / shares, 8 KV heads of 128, lengths from half of the rows up:
+//   1 sequence   1000 rows 7.4 / 9.6, 2000 9.4 / 9.4, 4000 13.3 / 10.8    12 sequences  1000 rows 14.7 / 17.5, 2000 24.1 / 23.3, 4000 41 / 34
+//   8 sequences  1000 rows 10.2 / 13.9, 4000 24.5 / 26.1, 8000 43 / 42     64 sequences  500 rows 26 / 30, 1000 43 / 45, 2000 77 / 73
+//   48 pages of 32 rows of 16000: 1 sequence 17.6 / 21.6, 4 20 / 26, 16 38 / 53; of 4000: 32 sequences 47 / 63, 48 89 / 87, 64 92 / 111
+//   64 pages of 64 rows of 131072: 1 sequence 29.7 / 25; of 32000: 22.9 / 23.1, 8 sequences 39 / 46
+// Longer rows than kPcMaxRows are cut into shares whatever they are, which balances lengths that differ much.
+constexpr int kPcMaxRows = 4096;
+int paged_cluster(const sablock_params_t* p, const Paged& pg, int n_sel)
+{
+    const int G = p->n_q_heads / p->n_kv_heads, dp = p->head_dim <= 64 ? 64 : 128;
+    if (p->dtype != SABLOCK_BF16 || G > 8 || p->head_dim > 128) return 0;
+    if (n_sel && (n_sel > kPcMaxList || pg.max_pages > pc_keys(dp))) return 0;
+    const long long pairs = (long long)pg.n_seqs * p->n_kv_heads, room = 2LL * sm_count();
+    const long long rows = n_sel ? (long long)(n_sel < pg.max_pages ? n_sel : pg.max_pages) * pg.page_size : pg.max_rows;
+    if (!n_sel && rows > kPcMaxRows) return 0;
+    int c = 1;
+    while (c < kPcMaxCluster && pairs * c * 2 <= room && rows > (long long)c * kPaUnit) c *= 2;
+    const long long used = pairs * c, places = (used + room - 1) / room * room;
+    const double bytes = (double)pairs * p->head_dim * 4 * (double)(rows + (n_sel ? pg.max_pages : 0));
+    return bytes * (double)(places - used) / (double)used <= (n_sel ? 80e6 : 40e6) ? c : 0;
+}
+
+// ps: how to choose the pages, where the call does; sel: the list that the call gives, or has had made.
 sablock_status_t run_paged_attention(const sablock_params_t* p, const Paged& pg, const void* q, const int* sel, int n_sel, float* out,
-                                     float* lse, void* ws, size_t ws_bytes, cudaStream_t st)
+                                     float* lse, void* ws, size_t ws_bytes, cudaStream_t st, const PageSelectArgs* ps = nullptr)
 {
     const PagedPlan pl = paged_plan(p);
     if (!ws || ws_bytes < pl.bytes) return SABLOCK_ERR_WORKSPACE_TOO_SMALL;
@@ -1169,6 +1203,16 @@ sablock_status_t run_paged_attention(const sablock_params_t* p, const Paged& pg,
     a.part = static_cast<float*>(ws);
     a.jobs = at<int4>(ws, pl.o_jobs);
     a.out = out; a.lse = lse;
+    if (const int c = ps || !sel ? paged_cluster(p, pg, ps ? n_sel : 0) : 0) {
+        const PageSelectArgs none = {};
+        const bool q4 = a.G <= 4;
+#define SAB_CLUSTER(DP) \
+        return ps ? (q4 ? launch_paged_cluster<true, DP, true>(a, *ps, c, st) : launch_paged_cluster<false, DP, true>(a, *ps, c, st)) \
+                  : (q4 ? launch_paged_cluster<true, DP, false>(a, none, c, st) : launch_paged_cluster<false, DP, false>(a, none, c, st))
+        if (pl.dp == 64) SAB_CLUSTER(64);
+        SAB_CLUSTER(128);
+#undef SAB_CLUSTER
+    }
     sablock_status_t rc = SABLOCK_ERR_UNSUPPORTED;
 #define SAB_PAGED(DP) \
     if (pl.dp == DP) { \
@@ -1192,8 +1236,7 @@ sablock_status_t launch_page_select(const PageSelectArgs& a, int cluster, cudaSt
     const dim3 grid(cluster, a.pg.n_seqs * a.Hkv);
 #define SAB_SELECT(N) \
     do { SAB_TRY(allow_smem<page_select_kernel<T, N>>(smem)); \
-         if (cluster > 8) cudaFuncSetAttribute(page_select_kernel<T, N>, cudaFuncAttributeNonPortableClusterSizeAllowed, 1); \
-         return launch(page_select_kernel<T, N>, grid, kPsThreads, smem, st, cluster, a, cluster); } while (0)
+         return launch(page_select_kernel<T, N>, grid, ps_threads(N), smem, st, cluster, a, cluster); } while (0)
     if (per <= 1) SAB_SELECT(1);
     if constexpr (sizeof(T) == 4)
         if (per > 2) SAB_SELECT(4);
@@ -1201,21 +1244,28 @@ sablock_status_t launch_page_select(const PageSelectArgs& a, int cluster, cudaSt
 #undef SAB_SELECT
 }
 
-sablock_status_t run_page_select(const sablock_params_t* p, const Paged& pg, const void* q, int n_sel, int n_first, int n_last, int* sel,
-                                 cudaStream_t st)
+sablock_status_t page_select_args(const sablock_params_t* p, const Paged& pg, const void* q, int n_sel, int n_first, int n_last, int* sel,
+                                  PageSelectArgs* out)
 {
     if (!pg.bounds || n_sel < 1 || n_first < 0 || n_last < 0 || n_first > n_sel || n_last > n_sel - n_first) return SABLOCK_ERR_INVALID_ARG;
     if (pg.max_pages > kPsMaxPages) return SABLOCK_ERR_UNSUPPORTED;
-    const long long pairs = (long long)pg.n_seqs * p->n_kv_heads;
-    if (pairs > 65535 || (long long)n_sel * pg.page_size > kPgMaxRows) return SABLOCK_ERR_UNSUPPORTED;
+    if ((long long)pg.n_seqs * p->n_kv_heads > 65535 || (long long)n_sel * pg.page_size > kPgMaxRows) return SABLOCK_ERR_UNSUPPORTED;
     PageSelectArgs a;
     a.pg = pg;
     a.q = q; a.sel = sel;
     a.H = p->n_q_heads; a.Hkv = p->n_kv_heads; a.G = a.H / a.Hkv; a.D = p->head_dim;
     a.n_sel = n_sel; a.n_first = n_first; a.n_last = n_last;
-    // CTAs that share a sequence's pages: while there are SMs for them and 128 pages (one turn of a CTA's warps) each
+    *out = a;
+    return SABLOCK_OK;
+}
+
+sablock_status_t run_page_select(const sablock_params_t* p, const PageSelectArgs& a, cudaStream_t st)
+{
+    const Paged& pg = a.pg;
+    const long long pairs = (long long)pg.n_seqs * a.Hkv;
+    // CTAs that share a sequence's pages: while two fit on every SM, of 128 pages (one turn of a CTA's warps) at least
     int c = 1;
-    while (c < kPsMaxCluster && pg.max_pages >= SAB_PS_PAGES * c && pairs * c * 2 <= SAB_PS_FILL * sm_count()) c *= 2;
+    while (c < kPsMaxCluster && pg.max_pages >= 256 * c && pairs * c * 2 <= 2LL * sm_count()) c *= 2;
     return p->dtype == SABLOCK_BF16 ? launch_page_select<__nv_bfloat16>(a, c, st) : launch_page_select<float>(a, c, st);
 }
 
@@ -1701,7 +1751,9 @@ sablock_status_t sablock_page_select(const sablock_params_t* p, const sablock_pa
     SAB_TRY(paged_args(p, pages, &pg));
     if (!q || !selected) return SABLOCK_ERR_INVALID_ARG;
     if (!aligned16(q)) return SABLOCK_ERR_UNSUPPORTED;
-    return run_page_select(p, pg, q, n_selected, n_first, n_last, selected, static_cast<cudaStream_t>(stream));
+    PageSelectArgs ps;
+    SAB_TRY(page_select_args(p, pg, q, n_selected, n_first, n_last, selected, &ps));
+    return run_page_select(p, ps, static_cast<cudaStream_t>(stream));
 }
 
 sablock_status_t sablock_paged_sparse_attention(const sablock_params_t* p, const sablock_pages_t* pages, const void* q, int n_selected,
@@ -1715,8 +1767,12 @@ sablock_status_t sablock_paged_sparse_attention(const sablock_params_t* p, const
     if (!aligned16(q)) return SABLOCK_ERR_UNSUPPORTED;
     if (!ws || ws_bytes < paged_plan(p).bytes) return SABLOCK_ERR_WORKSPACE_TOO_SMALL;
     if (!aligned16(ws)) return SABLOCK_ERR_INVALID_ARG;
-    SAB_TRY(run_page_select(p, pg, q, n_selected, n_first, n_last, selected, static_cast<cudaStream_t>(stream)));
-    return run_paged_attention(p, pg, q, selected, n_selected, out, lse, ws, ws_bytes, static_cast<cudaStream_t>(stream));
+    cudaStream_t st = static_cast<cudaStream_t>(stream);
+    PageSelectArgs ps;
+    SAB_TRY(page_select_args(p, pg, q, n_selected, n_first, n_last, selected, &ps));
+    if (paged_cluster(p, pg, n_selected)) return run_paged_attention(p, pg, q, nullptr, n_selected, out, lse, ws, ws_bytes, st, &ps);
+    SAB_TRY(run_page_select(p, ps, st));
+    return run_paged_attention(p, pg, q, selected, n_selected, out, lse, ws, ws_bytes, st);
 }
 
 sablock_status_t sablock_compress_layers_host(const sablock_params_t* p, int n_layers, int n_seqs, const void* h_q_win,

@@ -142,10 +142,12 @@ SHAPES = [(32, 8, 128, BF16), (8, 1, 128, BF16), (5, 1, 128, BF16), (12, 1, 128,
 LENS = [0, 1, 15, 16, 17, 33, 64, 65, 500, 1]
 
 
-def _check_attention(c, p, q, selected=None, lists=None, absent=(), scale=1.0):
+def _check_attention(c, p, q, selected=None, lists=None, absent=(), scale=1.0, call=None):
+    """The call (attention over all rows or the pages `selected`, unless another one is given) against the reference."""
     ref, ref_lse = R.attention(c, q, lists, absent)
     g = c.handle(p)
-    out, lse = B.paged_attention(p, g, q, selected=selected, want_lse=True)
+    call = call or (lambda: B.paged_attention(p, g, q, selected=selected, want_lse=True))
+    out, lse = call()
     top = max([float(c.v[c.rows(s, min(max(n, 0), c.max_pages * c.page))].double().abs().max()) for s, n in enumerate(c.lens.tolist()) if n > 0] or [1.0]) \
         if not absent else float(c.v.double().nan_to_num(0).abs().max())
     assert float((out.double() - ref).abs().max()) <= 2e-5 * scale * top
@@ -154,8 +156,7 @@ def _check_attention(c, p, q, selected=None, lists=None, absent=(), scale=1.0):
     assert bool((out[empty] == 0).all())
     if not bool(empty.all()):
         assert float((lse.double() - ref_lse)[~empty].abs().max()) <= 1e-4 * scale
-    assert torch.equal(out, B.paged_attention(p, g, q, selected=selected))          # fixed order
-    return out
+    assert torch.equal(out, call()[0])                                             # fixed order
 
 
 @pytest.mark.parametrize("H,Hkv,D,dtype", SHAPES)
@@ -260,9 +261,13 @@ def test_page_select_and_attention_over_it(H, Hkv, D, dtype, page, lens, n_sel, 
     want = [[R.choose(x, n_sel, n_first, n_last) for x in heads] for heads in R.scores(c, q)]
     sel = B.page_select(p, g, q, n_sel, n_first, n_last)
     assert sel.tolist() == [[x + [-1] * (n_sel - len(x)) for x in heads] for heads in want]
-    out = _check_attention(c, p, q, sel, want)
-    out2, sel2, lse2 = B.paged_sparse_attention(p, g, q, n_sel, n_first, n_last, want_lse=True)
-    assert torch.equal(sel, sel2) and torch.equal(out, out2) and lse2.shape == (len(lens), H)
+    _check_attention(c, p, q, sel, want)
+
+    def both():
+        out, chosen, lse = B.paged_sparse_attention(p, g, q, n_sel, n_first, n_last, want_lse=True)
+        assert torch.equal(chosen, sel)
+        return out, lse
+    _check_attention(c, p, q, None, want, call=both)
 
 
 def test_page_select_ties_infinities_and_missing_numbers():
