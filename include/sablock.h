@@ -339,10 +339,12 @@ sablock_status_t sablock_paged_append(const sablock_params_t *p, const sablock_p
  *  selected NULL (n_selected 0): every row.  Otherwise dev int32 [n_seqs, Hkv, n_selected]: for each KV head the pages of the sequence
  *  (0 for its first) whose rows count; of a sequence with fewer pages than n_selected as many entries are
  *  read as it has pages; entries outside the sequence (-1) count nothing, an entry that stands twice counts twice.
- *  A sequence without rows gets zeros and -inf.  Scratch from ws (sablock_paged_workspace_bytes, which depends on the heads, head_dim
- *  and dtype only; 0 on invalid arguments); nothing in it has to be set.  Accumulation is fp32 in an order that the
- *  lengths of the call fix. */
-size_t sablock_paged_workspace_bytes(const sablock_params_t *p, const sablock_pages_t *pages);
+ *  A sequence without rows gets zeros and -inf.  Scratch from ws; nothing in it has to be set.  Accumulation is fp32 in an order that
+ *  the lengths of the call fix.
+ * sablock_paged_workspace_bytes: the bytes of ws for a call over all rows (n_selected 0), for sablock_paged_sparse_attention with
+ *  n_selected pages, and for any call (n_selected -1, also the one for a given list); 0 on invalid arguments, 16 where the call
+ *  needs none (NULL will do then).  It depends on the sizes in *p and *pages, not on what is in the device arrays. */
+size_t sablock_paged_workspace_bytes(const sablock_params_t *p, const sablock_pages_t *pages, int n_selected);
 sablock_status_t sablock_paged_attention(const sablock_params_t *p, const sablock_pages_t *pages, const void *q,
                                          const int *selected, int n_selected, float *out, float *lse,
                                          void *ws, size_t ws_bytes, sablock_stream_t stream);

@@ -110,7 +110,7 @@ def _load(path: str):
     ll = C.c_longlong
     l.sablock_paged_append.argtypes = [vp, vp, ci, vp, vp, ll, vp, ll, vp, ll, vp, vp, vp, ci, ci, vp]
     l.sablock_paged_workspace_bytes.restype = sz
-    l.sablock_paged_workspace_bytes.argtypes = [vp, vp]
+    l.sablock_paged_workspace_bytes.argtypes = [vp, vp, ci]
     l.sablock_paged_attention.argtypes = [vp, vp, vp, vp, ci, vp, vp, vp, sz, vp]
     l.sablock_page_select.argtypes = [vp, vp, vp, ci, ci, ci, vp, vp]
     l.sablock_paged_sparse_attention.argtypes = [vp, vp, vp, ci, ci, ci, vp, vp, vp, vp, sz, vp]
@@ -121,6 +121,7 @@ def _load(path: str):
         fn = getattr(l, "sablock_" + name)
         setattr(l, name, _fastcall.bind(C.cast(fn, C.c_void_p).value) if _fastcall else fn)
     l.decode_step = _fastcall.bind_decode(C.cast(l.sablock_decode_attention, C.c_void_p).value) if _fastcall else None
+    l.append_step = (_fastcall.bind_append(C.cast(l.sablock_paged_append, C.c_void_p).value) if hasattr(_fastcall, "bind_append") else None)
     l.sablock_decode_workspace_bytes.restype = C.c_size_t
     l.sablock_decode_workspace_bytes.argtypes = [vp, ci, ci]
     l.sablock_decode_attention.argtypes = [vp, ci, vp, vp, vp, ci, vp, vp, vp, vp, sz, vp]
@@ -465,24 +466,29 @@ def make_pages(p: Params, k_pages: torch.Tensor, v_pages: torch.Tensor, table: t
     g._dtype, g._device, g._q_shape = dt, dev, (g.n_seqs, p.n_q_heads, d)
     # what the calls' outputs and scratch look like: empty_like of a tensor costs half of an empty
     g._lse_like = torch.empty(1, device=dev).expand(g.n_seqs, p.n_q_heads)
-    g._ws_like = torch.empty(1, dtype=torch.uint8, device=dev).expand(
-        max(16, int(lib().sablock_paged_workspace_bytes(C.addressof(p), C.addressof(g)))))
-    g._sel_like = {}
+    g._like = {}
+    # what the marshalling module checks an append against (there is no stream to enqueue on without a GPU)
+    g._fast = (dt, dev, g.n_seqs, hkv, p.n_q_heads, d, torch.int32, torch.float32, torch.empty_like) if dev.type == "cuda" else None
     return g
 
 
-def _selection(p: Params, pages: Pages, n: int) -> torch.Tensor:
-    like = pages._sel_like.get(n)
-    if like is None:
-        like = pages._sel_like[n] = torch.empty(1, dtype=torch.int32, device=pages._device).expand(pages.n_seqs, p.n_kv_heads, max(int(n), 0))
-    return torch.empty_like(like)
-
-
-def paged_workspace_bytes(p: Params, pages: Pages) -> int:
-    n = int(lib().sablock_paged_workspace_bytes(C.addressof(p), C.addressof(pages)))
+def paged_workspace_bytes(p: Params, pages: Pages, n_selected: int = -1) -> int:
+    """Scratch of a call over all rows (0), of paged_sparse_attention with n_selected pages, of any call (-1)."""
+    n = int(lib().sablock_paged_workspace_bytes(C.addressof(p), C.addressof(pages), n_selected))
     if n == 0:
         raise SablockError(2, "sablock_paged_workspace_bytes")
     return n
+
+
+def _like(p: Params, pages: Pages, n_selected: int):
+    """What the scratch (None where a call needs none) and the page list of such a call look like."""
+    like = pages._like.get(n_selected)
+    if like is None:
+        n, dev = paged_workspace_bytes(p, pages, n_selected), pages._device
+        like = pages._like[n_selected] = (
+            torch.empty(1, dtype=torch.uint8, device=dev).expand(n) if n > 16 else None,
+            torch.empty(1, dtype=torch.int32, device=dev).expand(pages.n_seqs, p.n_kv_heads, max(int(n_selected), 0)))
+    return like
 
 
 def paged_append(p: Params, pages: Pages, k: torch.Tensor, v: torch.Tensor, q: Optional[torch.Tensor] = None,
@@ -490,6 +496,14 @@ def paged_append(p: Params, pages: Pages, k: torch.Tensor, v: torch.Tensor, q: O
                  cu_new: Optional[torch.Tensor] = None, q_out: Optional[torch.Tensor] = None) -> Optional[torch.Tensor]:
     """New tokens k, v [n, Hkv, D] become the last rows of their sequences (cu_new int32 [n_seqs + 1]: whose they are; None: one
     each), keys and queries q [n, H, D] rotated by positions * inv_freq on the way.  Returns the rotated queries."""
+    l, fast = lib(), pages._fast
+    if l.append_step is not None and fast is not None:
+        done = l.append_step(C.addressof(p), C.addressof(pages), fast, k, v, q, q_out, positions, inv_freq, interleaved, cu_new, _stream())
+        if done is None or type(done) is torch.Tensor:
+            return done
+        if type(done) is int:
+            raise SablockError(done, "sablock_paged_append")
+    # (something does not fit, or the module is not there: the same again, step by step)
     dt, dev, hkv, H, d = pages._dtype, pages._device, p.n_kv_heads, p.n_q_heads, p.head_dim
     n = k.shape[0]
     ks, vs, qs, q_at, out_at = _tokens("k", k, dt, dev, n, hkv, d), _tokens("v", v, dt, dev, n, hkv, d), 0, None, None
@@ -508,7 +522,7 @@ def paged_append(p: Params, pages: Pages, k: torch.Tensor, v: torch.Tensor, q: O
         rotary = 2 * inv_freq.shape[0]
         freq_at = _contiguous("inv_freq", inv_freq, torch.float32, dev, (rotary // 2,))
     cu_at = None if cu_new is None else _contiguous("cu_new", cu_new, torch.int32, dev, (pages.n_seqs + 1,))
-    code = lib().paged_append(C.addressof(p), C.addressof(pages), n, cu_at, k.data_ptr(), ks, v.data_ptr(), vs, q_at, qs, out_at, pos_at,
+    code = l.paged_append(C.addressof(p), C.addressof(pages), n, cu_at, k.data_ptr(), ks, v.data_ptr(), vs, q_at, qs, out_at, pos_at,
                               freq_at, rotary, 1 if interleaved else 0, _stream())
     if code != OK:
         raise SablockError(code, "sablock_paged_append")
@@ -527,9 +541,10 @@ def paged_attention(p: Params, pages: Pages, q: torch.Tensor, selected: Optional
     out = torch.empty_like(q, dtype=torch.float32)
     lse = torch.empty_like(pages._lse_like) if want_lse else None
     if ws is None:
-        ws = torch.empty_like(pages._ws_like)
+        like = _like(p, pages, 0 if selected is None else -1)[0]
+        ws = None if like is None else torch.empty_like(like)
     code = lib().paged_attention(C.addressof(p), C.addressof(pages), q_at, sel_at, n, out.data_ptr(), lse.data_ptr() if want_lse else None,
-                                 ws.data_ptr(), ws.numel(), _stream())
+                                 None if ws is None else ws.data_ptr(), 0 if ws is None else ws.numel(), _stream())
     if code != OK:
         raise SablockError(code, "sablock_paged_attention")
     return (out, lse) if want_lse else out
@@ -538,7 +553,7 @@ def paged_attention(p: Params, pages: Pages, q: torch.Tensor, selected: Optional
 def page_select(p: Params, pages: Pages, q: torch.Tensor, n_selected: int, n_first: int = 1, n_last: int = 1) -> torch.Tensor:
     """The pages whose bounds promise the largest logits, per KV head: int32 [n_seqs, Hkv, n_selected], ascending, then -1."""
     q_at = _contiguous("q", q, pages._dtype, pages._device, pages._q_shape)
-    selected = _selection(p, pages, n_selected)
+    selected = torch.empty_like(_like(p, pages, n_selected)[1])
     _check(lib().page_select(C.addressof(p), C.addressof(pages), q_at, n_selected, n_first, n_last, _ptr(selected), _stream()),
            "sablock_page_select")
     return selected
@@ -550,11 +565,13 @@ def paged_sparse_attention(p: Params, pages: Pages, q: torch.Tensor, n_selected:
     q_at = _contiguous("q", q, pages._dtype, pages._device, pages._q_shape)
     out = torch.empty_like(q, dtype=torch.float32)
     lse = torch.empty_like(pages._lse_like) if want_lse else None
-    if ws is None:
-        ws = torch.empty_like(pages._ws_like)
-    selected = _selection(p, pages, n_selected)
+    ws_like, sel_like = _like(p, pages, n_selected)
+    selected = torch.empty_like(sel_like)
+    if ws is None and ws_like is not None:
+        ws = torch.empty_like(ws_like)
     code = lib().paged_sparse_attention(C.addressof(p), C.addressof(pages), q_at, n_selected, n_first, n_last, selected.data_ptr(),
-                                        out.data_ptr(), lse.data_ptr() if want_lse else None, ws.data_ptr(), ws.numel(), _stream())
+                                        out.data_ptr(), lse.data_ptr() if want_lse else None, None if ws is None else ws.data_ptr(),
+                                        0 if ws is None else ws.numel(), _stream())
     if code != OK:
         raise SablockError(code, "sablock_paged_sparse_attention")
     return (out, selected, lse) if want_lse else (out, selected)

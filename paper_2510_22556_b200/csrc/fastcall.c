@@ -189,36 +189,135 @@ static int take_three(PyObject* t, long long (*x)[3])
     return 1;
 }
 
+/* 1: t is a contiguous tensor of that type, device and n elements in one dimension; 0: it is not; -1: an error. */
+static int fits_vector(PyObject* t, PyObject* dtype, PyObject* device, long long n)
+{
+    int rc = attr_equals(t, s_dtype, dtype);
+    if (rc == 1) rc = attr_equals(t, s_device, device);
+    if (rc != 1) return rc;
+    PyObject* x = PyObject_GetAttr(t, s_shape);
+    if (!x) return -1;
+    rc = PyTuple_Check(x) && PyTuple_GET_SIZE(x) == 1 && (n < 0 || PyLong_AsLongLong(PyTuple_GET_ITEM(x, 0)) == n);
+    Py_DECREF(x);
+    if (rc != 1) return rc;
+    x = PyObject_CallMethodNoArgs(t, s_contiguous);
+    if (!x) return -1;
+    rc = x == Py_True;
+    Py_DECREF(x);
+    return rc;
+}
+
+/* What token_stride says, for a type, a device and sizes that are at hand; -2: an error. */
+static long long stride_of(PyObject* t, PyObject* dtype, PyObject* device, long long n, long long heads, long long d)
+{
+    long long size[3], stride[3];
+    int rc = attr_equals(t, s_dtype, dtype);
+    if (rc == 1) rc = attr_equals(t, s_device, device);
+    if (rc == 1) {
+        PyObject* x = PyObject_GetAttr(t, s_shape);
+        if (!x) return -2;
+        rc = take_three(x, &size);
+        Py_DECREF(x);
+    }
+    if (rc == 1) rc = size[0] == n && size[1] == heads && size[2] == d;
+    if (rc == 1) {
+        PyObject* x = PyObject_CallMethodNoArgs(t, s_stride);
+        if (!x) return -2;
+        rc = take_three(x, &stride);
+        Py_DECREF(x);
+    }
+    if (rc < 0) return -2;
+    if (rc == 1 && n > 0) rc = (d < 2 || stride[2] == 1) && (heads < 2 || stride[1] == d);
+    return rc != 1 ? -1 : n > 1 ? stride[0] : 0;
+}
+
 static PyObject* token_stride(PyObject* module, PyObject* const* args, Py_ssize_t n)
 {
     (void)module;
-    long long want[3], size[3], stride[3];
+    long long want[3];
     if (n != 6) return PyErr_Format(PyExc_TypeError, "%zd arguments, not 6", n);
     for (int i = 0; i < 3; ++i) {
         want[i] = PyLong_AsLongLong(args[3 + i]);
         if (want[i] == -1 && PyErr_Occurred()) return NULL;
     }
-    int rc = attr_equals(args[0], s_dtype, args[1]);
-    if (rc == 1) rc = attr_equals(args[0], s_device, args[2]);
-    if (rc == 1) {
-        PyObject* x = PyObject_GetAttr(args[0], s_shape);
-        if (!x) return NULL;
-        rc = take_three(x, &size);
-        Py_DECREF(x);
-    }
-    if (rc == 1) rc = size[0] == want[0] && size[1] == want[1] && size[2] == want[2];
-    if (rc == 1) {
-        PyObject* x = PyObject_CallMethodNoArgs(args[0], s_stride);
-        if (!x) return NULL;
-        rc = take_three(x, &stride);
-        Py_DECREF(x);
-    }
-    if (rc < 0) return NULL;
-    if (rc == 1 && size[0] > 0) rc = (size[2] < 2 || stride[2] == 1) && (size[1] < 2 || stride[1] == size[2]);
-    return PyLong_FromLongLong(rc != 1 ? -1 : size[0] > 1 ? stride[0] : 0);
+    const long long s = stride_of(args[0], args[1], args[2], want[0], want[1], want[2]);
+    return s == -2 ? NULL : PyLong_FromLongLong(s);
 }
 
-static PyMethodDef methods[] = {{"fits", (PyCFunction)(void (*)(void))fits, METH_FASTCALL, "fits(tensor, dtype, device, shape)"},
+/* Appending is one short call per layer and token: bind_append(address) returns a builtin that takes the tensors themselves,
+ * (params, pages, (dtype, device, n_seqs, n_kv_heads, n_q_heads, head_dim, int32, float32, empty_like), k, v, q, q_out, positions,
+ * inv_freq, interleaved, cu_new, stream), checks them and calls sablock_paged_append.  It returns the rotated queries (None without
+ * queries), a status code that is not 0, or NotImplemented where an argument does not fit: the caller says then which. */
+static PyObject* invoke_append(PyObject* self, PyObject* const* args, Py_ssize_t n_args)
+{
+    typedef int (*append)(u, u, u, u, u, u, u, u, u, u, u, u, u, u, u, u);
+    u p = 0, pages = 0, k = 0, v = 0, q = 0, out = 0, pos = 0, freq = 0, cu = 0, stream = 0, n = 0, rotary = 0;
+    long long want[4], ks, vs, qs = 0;
+    if (n_args != 12) return PyErr_Format(PyExc_TypeError, "%zd arguments, not 12", n_args);
+    PyObject* spec = args[2];
+    if (!PyTuple_Check(spec) || PyTuple_GET_SIZE(spec) != 9) return PyErr_Format(PyExc_TypeError, "a description of nine parts");
+    PyObject *dtype = PyTuple_GET_ITEM(spec, 0), *device = PyTuple_GET_ITEM(spec, 1), *i32 = PyTuple_GET_ITEM(spec, 6), *f32 = PyTuple_GET_ITEM(spec, 7);
+    for (int i = 0; i < 4; ++i) {
+        want[i] = PyLong_AsLongLong(PyTuple_GET_ITEM(spec, 2 + i));
+        if (want[i] == -1 && PyErr_Occurred()) return NULL;
+    }
+    const long long seqs = want[0], hkv = want[1], heads = want[2], d = want[3];
+    if (take_scalar(args[0], &p) < 0 || take_scalar(args[1], &pages) < 0 || take_scalar(args[11], &stream) < 0 || take_extent(args[3], 3, 0, &n) < 0) {
+        if (PyErr_ExceptionMatches(PyExc_ValueError) || PyErr_ExceptionMatches(PyExc_AttributeError)) {      /* no tensor of three dimensions */
+            PyErr_Clear();
+            Py_RETURN_NOTIMPLEMENTED;
+        }
+        return NULL;
+    }
+    const int turned = PyObject_IsTrue(args[9]);
+    if (turned < 0) return NULL;
+    const int has_q = args[5] != Py_None, made = has_q && args[6] == Py_None;
+    int rc = (ks = stride_of(args[3], dtype, device, (long long)n, hkv, d)) >= 0 && (vs = stride_of(args[4], dtype, device, (long long)n, hkv, d)) >= 0;
+    if (rc && has_q) rc = (qs = stride_of(args[5], dtype, device, (long long)n, heads, d)) >= 0;
+    if (rc && !made) rc = args[6] == Py_None;        /* (a caller's own buffer takes the other way) */
+    if (rc && args[7] != Py_None) rc = fits_vector(args[7], i32, device, (long long)n) == 1;
+    if (rc && args[8] != Py_None) {
+        rc = fits_vector(args[8], f32, device, -1) == 1 && take_extent(args[8], 1, 0, &rotary) == 0;
+        rotary *= 2;
+    }
+    if (rc && args[10] != Py_None) rc = fits_vector(args[10], i32, device, seqs + 1) == 1;
+    if (!rc) {
+        PyErr_Clear();
+        Py_RETURN_NOTIMPLEMENTED;
+    }
+    PyObject* result = Py_NewRef(Py_None);
+    if (made) {
+        Py_DECREF(result);
+        result = PyObject_CallOneArg(PyTuple_GET_ITEM(spec, 8), args[5]);      /* (contiguous: tokens apart are not kept apart) */
+        if (!result) return NULL;
+    }
+    if (take_method(args[3], s_data_ptr, &k) < 0 || take_method(args[4], s_data_ptr, &v) < 0 || take_method(args[5], s_data_ptr, &q) < 0 ||
+        take_method(result, s_data_ptr, &out) < 0 || take_method(args[7], s_data_ptr, &pos) < 0 || take_method(args[8], s_data_ptr, &freq) < 0 ||
+        take_method(args[10], s_data_ptr, &cu) < 0) {
+        Py_DECREF(result);
+        return NULL;
+    }
+    const append f = (append)(uintptr_t)PyLong_AsUnsignedLongLong(self);
+    int code;
+    Py_BEGIN_ALLOW_THREADS
+    code = f(p, pages, n, cu, k, (u)ks, v, (u)vs, q, (u)qs, out, pos, freq, rotary, (u)turned, stream);
+    Py_END_ALLOW_THREADS
+    if (code == 0) return result;
+    Py_DECREF(result);
+    return PyLong_FromLong(code);
+}
+
+static PyMethodDef invoke_append_def = {"append", (PyCFunction)(void (*)(void))invoke_append, METH_FASTCALL, "calls sablock_paged_append"};
+
+static PyObject* bind_append(PyObject* module, PyObject* address)
+{
+    (void)module;
+    if (!PyLong_Check(address)) return PyErr_Format(PyExc_TypeError, "an address");
+    return PyCFunction_New(&invoke_append_def, address);
+}
+
+static PyMethodDef methods[] = {{"bind_append", bind_append, METH_O, "bind_append(address): sablock_paged_append for tensors"},
+                                {"fits", (PyCFunction)(void (*)(void))fits, METH_FASTCALL, "fits(tensor, dtype, device, shape)"},
                                 {"token_stride", (PyCFunction)(void (*)(void))token_stride, METH_FASTCALL,
                                  "token_stride(tensor, dtype, device, n, heads, channels)"},
                                 {"bind_decode", bind_decode, METH_O, "bind_decode(address): sablock_decode_attention for tensors"},

@@ -223,6 +223,10 @@ __host__ __device__ constexpr int pa_ring_bytes(int DP) { return kPaWarps * kPaS
 __host__ __device__ constexpr int pa_smem(int DP, int heads) { return pa_ring_bytes(DP) + kPaWarps * 4 * DP * (int)sizeof(float) + heads * (DP + 8) * 2; }
 static_assert(2 * (pa_smem(128, 16) + 512 + 1024) <= kSmSharedBytes, "two CTAs on an SM");
 
+__device__ __forceinline__ void ldsm_x2(uint32_t addr, uint32_t& r0, uint32_t& r1)
+{
+    asm volatile("ldmatrix.sync.aligned.m8n8.x2.shared.b16 {%0, %1}, [%2];" : "=r"(r0), "=r"(r1) : "r"(addr) : "memory");
+}
 // The product alone, nothing added.
 __device__ __forceinline__ void mma_bf16_only(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1)
 {
@@ -239,7 +243,9 @@ template <int NS, bool Q4, int DP> struct PaWarp {
     static constexpr uint32_t kOp = 16 * DP * 2;     // bytes of a chunk of K or V
     using Queries = __nv_bfloat16 (*)[DP + 8];
     using Sums = float (*)[4][DP];
-    uint32_t qa[KS][2 * NS];
+    static constexpr bool kKeep = KS * NS <= 8;      // the queries stay in registers; more are read from shared memory at every chunk
+    uint32_t qa[kKeep ? KS : 1][2 * NS];
+    uint32_t q_at;
     float m[NS], l[NS];
     uint64_t acc[NS][DP / 8][2];                     // packed pairs
 
@@ -255,15 +261,19 @@ template <int NS, bool Q4, int DP> struct PaWarp {
     }
     __device__ __forceinline__ void take_queries(Queries qs, int lane)
     {
+        // row of matrix lane / 8: heads 0-7 and, with two sets, 8-15 of the first eight channels of a k-step, then of the others
+        const int mat = lane >> 3, row = Q4 ? lane & 3 : NS == 2 ? (lane & 7) + 8 * (mat & 1) : lane & 7;
+        q_at = smem_u32(&qs[row][8 * (NS == 2 ? mat >> 1 : mat & 1)]);
+        if constexpr (kKeep)
 #pragma unroll
-        for (int n = 0; n < NS; ++n) {
-            const int hh = Q4 ? (lane >> 2) & 3 : 8 * n + (lane >> 2);
+            for (int n = 0; n < NS; ++n) {
+                const int hh = Q4 ? (lane >> 2) & 3 : 8 * n + (lane >> 2);
 #pragma unroll
-            for (int ks = 0; ks < KS; ++ks)
+                for (int ks = 0; ks < KS; ++ks)
 #pragma unroll
-                for (int x = 0; x < 2; ++x)
-                    qa[ks][2 * n + x] = *reinterpret_cast<const uint32_t*>(&qs[hh][ks * 16 + x * 8 + 2 * (lane & 3)]);
-        }
+                    for (int x = 0; x < 2; ++x)
+                        qa[ks][2 * n + x] = *reinterpret_cast<const uint32_t*>(&qs[hh][ks * 16 + x * 8 + 2 * (lane & 3)]);
+            }
     }
     // Sixteen rows of K and V at ks_base and vs_base, `there`: which of them exist.
     __device__ __forceinline__ void chunk(uint32_t ks_base, uint32_t vs_base, uint32_t there, float c2, int lane)
@@ -281,9 +291,20 @@ template <int NS, bool Q4, int DP> struct PaWarp {
             for (int ks = 0; ks < KS; ++ks) {
                 uint32_t b[4];
                 ldsm_x4(base + (uint32_t)((2 * ks + (mat & 1)) ^ lr) * 16, b);
-                const uint32_t a1 = NS == 2 ? qa[ks][2 * NS - 2] : 0u, a3 = NS == 2 ? qa[ks][2 * NS - 1] : 0u;
-                mma_bf16(c[0], qa[ks][0], a1, qa[ks][1], a3, b[0], b[1]);
-                mma_bf16(c[1], qa[ks][0], a1, qa[ks][1], a3, b[2], b[3]);
+                uint32_t a0, a1 = 0u, a2, a3 = 0u;
+                if constexpr (kKeep) {
+                    a0 = qa[ks][0];
+                    a2 = qa[ks][1];
+                    if constexpr (NS == 2) { a1 = qa[ks][2]; a3 = qa[ks][3]; }
+                } else if constexpr (NS == 2) {
+                    uint32_t q[4];
+                    ldsm_x4(q_at + ks * 32, q);
+                    a0 = q[0]; a1 = q[1]; a2 = q[2]; a3 = q[3];
+                } else {
+                    ldsm_x2(q_at + ks * 32, a0, a2);
+                }
+                mma_bf16(c[0], a0, a1, a2, a3, b[0], b[1]);
+                mma_bf16(c[1], a0, a1, a2, a3, b[2], b[3]);
             }
         }
         // logits of this thread's heads, rows row0, row0 + 1, row0 + 8, row0 + 9 of the chunk
@@ -446,8 +467,11 @@ template <int GP, int DP> struct PaQueries {
     }
 };
 
+// CTAs on an SM: what shared memory holds.  (Three with 64 channels were no faster: 16 sequences of 4K to 16K rows 63 and 61 us.)
+__host__ __device__ constexpr int pa_per_sm(int DP) { return DP == 256 ? 1 : 2; }
+
 template <int NS, bool Q4, int DP>
-__global__ void __launch_bounds__(kPaThreads, DP == 256 ? 1 : 2)
+__global__ void __launch_bounds__(kPaThreads, pa_per_sm(DP))
 paged_mma_kernel(const __grid_constant__ PagedAttnArgs a)
 {
     using Warp = PaWarp<NS, Q4, DP>;

@@ -1123,11 +1123,12 @@ PagedPlan paged_plan(const sablock_params_t* p)
     PagedPlan pl;
     const int G = p->n_q_heads / p->n_kv_heads;
     pl.dp = p->head_dim <= 64 ? 64 : p->head_dim <= 128 ? 128 : 256;
-    // Heads of a KV head that go through a CTA together; more are groups, which read the rows again
+    // Heads of a KV head that go through a CTA together; more are groups, which read the rows again (16 heads as two groups of eight:
+    // 197 us where one takes 160)
     const int most = p->dtype == SABLOCK_BF16 && pl.dp <= 128 ? 16 : 8;
     pl.group_heads = G <= 4 ? 4 : G <= 8 || most == 8 ? 8 : 16;
     pl.groups = (G + pl.group_heads - 1) / pl.group_heads;
-    int ctas = (pl.dp == 256 ? 1 : 2) * sm_count();
+    int ctas = pa_per_sm(pl.dp) * sm_count();
     if (ctas > kPmMaxParts) ctas = kPmMaxParts;
     // Columns of heads: a divisor of theirs, up to 16, that leaves the fewest CTAs without work; the most columns of those
     const int all = p->n_kv_heads * pl.groups;
@@ -1191,8 +1192,11 @@ sablock_status_t run_paged_attention(const sablock_params_t* p, const Paged& pg,
                                      float* lse, void* ws, size_t ws_bytes, cudaStream_t st, const PageSelectArgs* ps = nullptr)
 {
     const PagedPlan pl = paged_plan(p);
-    if (!ws || ws_bytes < pl.bytes) return SABLOCK_ERR_WORKSPACE_TOO_SMALL;
-    if (!aligned16(ws)) return SABLOCK_ERR_INVALID_ARG;
+    const int c = ps || !sel ? paged_cluster(p, pg, n_sel) : 0;
+    if (!c) {                                        // (one launch needs no scratch)
+        if (!ws || ws_bytes < pl.bytes) return SABLOCK_ERR_WORKSPACE_TOO_SMALL;
+        if (!aligned16(ws)) return SABLOCK_ERR_INVALID_ARG;
+    }
     PagedAttnArgs a;
     a.pg = pg;
     a.q = q; a.sel = sel; a.n_sel = n_sel;
@@ -1203,7 +1207,7 @@ sablock_status_t run_paged_attention(const sablock_params_t* p, const Paged& pg,
     a.part = static_cast<float*>(ws);
     a.jobs = at<int4>(ws, pl.o_jobs);
     a.out = out; a.lse = lse;
-    if (const int c = ps || !sel ? paged_cluster(p, pg, ps ? n_sel : 0) : 0) {
+    if (c) {
         const PageSelectArgs none = {};
         const bool q4 = a.G <= 4;
 #define SAB_CLUSTER(DP) \
@@ -1726,10 +1730,11 @@ sablock_status_t sablock_paged_append(const sablock_params_t* p, const sablock_p
                 : launch(paged_bounds_kernel<float>, pages_grid, kApThreads, 0, st, 1, a);
 }
 
-size_t sablock_paged_workspace_bytes(const sablock_params_t* p, const sablock_pages_t* pages)
+size_t sablock_paged_workspace_bytes(const sablock_params_t* p, const sablock_pages_t* pages, int n_selected)
 {
     Paged pg;
-    return paged_args(p, pages, &pg) == SABLOCK_OK ? paged_plan(p).bytes : 0;
+    if (paged_args(p, pages, &pg) != SABLOCK_OK) return 0;
+    return n_selected >= 0 && paged_cluster(p, pg, n_selected) ? 16 : paged_plan(p).bytes;
 }
 
 sablock_status_t sablock_paged_attention(const sablock_params_t* p, const sablock_pages_t* pages, const void* q, const int* selected,
@@ -1765,12 +1770,12 @@ sablock_status_t sablock_paged_sparse_attention(const sablock_params_t* p, const
     SAB_TRY(paged_args(p, pages, &pg));
     if (!q || !selected || !out) return SABLOCK_ERR_INVALID_ARG;
     if (!aligned16(q)) return SABLOCK_ERR_UNSUPPORTED;
-    if (!ws || ws_bytes < paged_plan(p).bytes) return SABLOCK_ERR_WORKSPACE_TOO_SMALL;
-    if (!aligned16(ws)) return SABLOCK_ERR_INVALID_ARG;
     cudaStream_t st = static_cast<cudaStream_t>(stream);
     PageSelectArgs ps;
     SAB_TRY(page_select_args(p, pg, q, n_selected, n_first, n_last, selected, &ps));
     if (paged_cluster(p, pg, n_selected)) return run_paged_attention(p, pg, q, nullptr, n_selected, out, lse, ws, ws_bytes, st, &ps);
+    if (!ws || ws_bytes < paged_plan(p).bytes) return SABLOCK_ERR_WORKSPACE_TOO_SMALL;      // (before the first launch)
+    if (!aligned16(ws)) return SABLOCK_ERR_INVALID_ARG;
     SAB_TRY(run_page_select(p, ps, st));
     return run_paged_attention(p, pg, q, selected, n_selected, out, lse, ws, ws_bytes, st);
 }

@@ -73,7 +73,7 @@ def _call(l, name, p, g, **kw):
 def test_caches_that_every_call_refuses(lib, params, pages, code):
     p, g = _params(**params), _pages(**pages)
     assert [_call(lib, name, p, g) for name in NAMES] == [code] * 4
-    assert lib.sablock_paged_workspace_bytes(C.addressof(p), C.addressof(g)) == 0
+    assert lib.sablock_paged_workspace_bytes(C.addressof(p), C.addressof(g), -1) == 0
 
 
 def test_null_blocks(lib):
@@ -91,7 +91,7 @@ def test_null_blocks(lib):
     (dict(sel=None), ["attend", "select", "sparse"], INVALID), (dict(first=-1), ["select", "sparse"], INVALID),
     (dict(first=3, last=2), ["select", "sparse"], INVALID), (dict(last=1 << 30), ["select", "sparse"], INVALID),
     (dict(n_sel=1 << 30), ["attend", "select", "sparse"], UNSUPPORTED),
-    (dict(ws=None), ["attend", "sparse"], TOO_SMALL), (dict(ws_bytes=64), ["attend", "sparse"], TOO_SMALL), (dict(ws=FAKE + 8), ["attend", "sparse"], INVALID),
+    (dict(ws=None), ["attend"], TOO_SMALL), (dict(ws_bytes=64), ["attend"], TOO_SMALL), (dict(ws=FAKE + 8), ["attend"], INVALID),
 ])
 def test_arguments_that_are_refused(lib, kw, who, code):
     for name in who:
@@ -104,6 +104,20 @@ def test_selection_needs_bounds_and_a_table_that_fits(lib):
     for g, code in ((_pages(bounds=None), INVALID), (_pages(max_pages=49153, page_size=16), UNSUPPORTED)):
         assert lib.page_select(P, C.addressof(g), FAKE, 4, 1, 1, FAKE, None) == code
         assert lib.paged_sparse_attention(P, C.addressof(g), FAKE, 4, 1, 1, FAKE, FAKE, None, FAKE, 1 << 40, None) == code
+
+
+def test_scratch(lib):
+    """Short rows and chosen pages go out in one launch without scratch; long ones, fp32, a list that is given need it."""
+    p = _params()
+    short, long_, f32 = _pages(), _pages(max_pages=2000, page_size=64), _params(dtype=torch.float32)
+    need = lambda q, g, n: int(lib.sablock_paged_workspace_bytes(C.addressof(q), C.addressof(g), n))  # noqa: E731
+    full = need(p, short, -1)
+    assert full > 1 << 20 and need(p, short, 0) == 16 and need(p, long_, 0) == full == need(p, long_, -1)
+    assert need(p, _pages(n_seqs=16, max_pages=500, page_size=32), 48) == 16 and need(p, _pages(n_seqs=1, max_pages=2049), 64) == full
+    assert need(p, short, 2000) == full and need(f32, short, 0) > 16 and need(f32, short, 4) > 16
+    for g, kw, code in ((long_, dict(ws=None), TOO_SMALL), (long_, dict(ws_bytes=full - 1), TOO_SMALL), (long_, dict(ws=FAKE + 8), INVALID)):
+        assert _call(lib, "attend", p, g, sel=None, n_sel=0, **kw) == code == _call(lib, "sparse", p, _pages(n_seqs=1, max_pages=2049), n_sel=64, **kw)
+    assert B.last_launch_count() == 0
 
 
 def test_appending_nothing_is_no_error(lib):
@@ -127,7 +141,7 @@ def test_make_pages_reads_strides_off_the_tensors(lib):
     assert (g.k, g.v, g.table) == (k.data_ptr(), v.data_ptr(), table.data_ptr())
     assert (g.k_stride_page, g.k_stride_row, g.k_stride_head) == (256, 16, 64) == (g.v_stride_page, g.v_stride_row, g.v_stride_head)
     assert (g.n_seqs, g.n_pages, g.page_size, g.max_pages, g.table_stride) == (2, 6, 4, 3, 5)
-    assert B.paged_workspace_bytes(p, g) > 0
+    assert B.paged_workspace_bytes(p, g) > 16
 
 
 def test_make_pages_refuses(lib):
