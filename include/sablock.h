@@ -321,11 +321,12 @@ size_t sablock_pages_sizeof(void);   /* sizeof(sablock_pages_t) as the library w
  *  k, v dev [n_tokens, Hkv, D], q dev [n_tokens, H, D] or NULL, heads contiguous, tokens k_stride, v_stride, q_stride elements apart (0 =
  *  contiguous; so the parts of one projection's output can be passed in); q_out dev [n_tokens, H, D] contiguous, not
  *  overlapping q; NULL with q.
- *  inv_freq dev f32[rotary_dim / 2] or NULL (rotary_dim = 0: no rotation; how rows that the compression retained, which are
+ *  k, v and q lie outside the pools.
+ *  inv_freq dev f32[rotary_dim / 2], finite, or NULL (rotary_dim = 0: no rotation; how rows that the compression retained, which are
  *  rotated already, go into pages): the first rotary_dim channels of a head are turned in pairs (i, i + rotary_dim / 2), or
  *  (2 i, 2 i + 1) with interleaved, by the angle position * inv_freq[i].  positions dev int32[n_tokens] or NULL (the
  *  row number).  After a compression a token's position is not its row: pass positions.
- *  The angle is formed in double and the rotation computed in fp32, rounded once to dtype.
+ *  The angle is formed in 64 bits modulo a turn, the rotation computed in fp32 and rounded once to dtype.
  *  With bounds: those of the pages that rows fall into are brought up to date; the first row of a page starts them anew.  Bounds hold no number
  *  where a key does not. */
 sablock_status_t sablock_paged_append(const sablock_params_t *p, const sablock_pages_t *pages, int n_tokens,
@@ -349,7 +350,7 @@ sablock_status_t sablock_paged_attention(const sablock_params_t *p, const sabloc
                                          const int *selected, int n_selected, float *out, float *lse,
                                          void *ws, size_t ws_bytes, sablock_stream_t stream);
 
-/* Which pages a token's queries should look at: for each KV head the n_selected pages whose bounds promise the largest logits,
+/* Which pages a token's queries should look at: for each KV head the n_selected pages whose bounds (required) promise the largest logits,
  *   score(page) = sum over the head's queries h and channels d of max(q[h][d] * lo[d], q[h][d] * hi[d]),
  * in double, rounded once to fp32; ties go to the lower page.  The first n_first and the last n_last pages of a sequence are always
  * in (n_first + n_last <= n_selected).  A score that is no number ranks above all others, a page that is not followed below.
@@ -359,7 +360,8 @@ sablock_status_t sablock_page_select(const sablock_params_t *p, const sablock_pa
                                      int n_selected, int n_first, int n_last, int *selected,
                                      sablock_stream_t stream);
 
-/* Both: the attention over the pages that sablock_page_select chooses, which are left in selected. */
+/* Both: the attention over the pages that sablock_page_select chooses, which are left in selected.  (The sums may be added up in
+ * another order than sablock_paged_attention with that list adds them.) */
 sablock_status_t sablock_paged_sparse_attention(const sablock_params_t *p, const sablock_pages_t *pages, const void *q,
                                                 int n_selected, int n_first, int n_last, int *selected,
                                                 float *out, float *lse, void *ws, size_t ws_bytes,

@@ -442,3 +442,88 @@ def test_refusals_on_the_gpu_leave_a_usable_context():
         with pytest.raises(B.SablockError):
             call()
     _check_attention(c, p, q)
+
+
+def test_calls_on_two_streams_at_once():
+    """Nothing is shared between calls: two caches decoded on two streams at the same time, with and without scratch, say what they say alone."""
+    p = _params(32, 8, 128, BF16)
+    caches = [Cache([9000, 700], 8, 128, 64, BF16, seed=1, bounds=True).fill(), Cache([12000, 40, 3000], 8, 128, 32, BF16, seed=2, bounds=True).fill()]
+    handles, qs = [c.handle(p) for c in caches], [c.randn(c.n_seqs, 32, 128) for c in caches]
+
+    def both(i):
+        return B.paged_attention(p, handles[i], qs[i]), *B.paged_sparse_attention(p, handles[i], qs[i], 12)
+    alone = [both(i) for i in range(2)]
+    torch.cuda.synchronize()
+    streams, got = [torch.cuda.Stream() for _ in range(2)], [[], []]
+    for _ in range(20):
+        for i in range(2):
+            with torch.cuda.stream(streams[i]):
+                got[i].append(both(i))
+    torch.cuda.synchronize()
+    for i in range(2):
+        assert all(torch.equal(a, b) for one in got[i] for a, b in zip(one, alone[i]))
+
+
+def test_a_cache_on_another_device_than_the_current_one_is_refused():
+    p = _params(4, 2, 16, F32)
+    c = Cache([5], 2, 16, 4, F32, bounds=True).fill()
+    g = c.handle(p)
+    g._index += 1                                             # as if it were on the next GPU
+    x, q = c.randn(1, 2, 16), c.randn(1, 4, 16)
+    for call in (lambda: B.paged_append(p, g, x, x), lambda: B.paged_attention(p, g, q), lambda: B.page_select(p, g, q, 2),
+                 lambda: B.paged_sparse_attention(p, g, q, 2)):
+        with pytest.raises(ValueError):
+            call()
+
+
+def test_append_through_ctypes_and_through_the_module():
+    """The binding without its marshalling module, and a caller's own buffer for the queries, do the same."""
+    p = _params(8, 2, 64, BF16)
+    outs = []
+    for slow, own in ((False, False), (True, False), (False, True)):
+        c = Cache([40, 9], 2, 64, 16, BF16, seed=4, bounds=True, fill=0.0)
+        g = c.handle(p)
+        if slow:
+            g._fast = None
+        qkv = c.randn(7, 12, 64)
+        buf = torch.empty(7, 8, 64, dtype=BF16, device="cuda") if own else None
+        freq = torch.linspace(1.0, 0.001, 32, device="cuda")
+        q = B.paged_append(p, g, qkv[:, 8:10], qkv[:, 10:], q=qkv[:, :8], inv_freq=freq, cu_new=torch.tensor([0, 4, 7], dtype=torch.int32, device="cuda"),
+                           positions=torch.arange(7, dtype=torch.int32, device="cuda") * 9, q_out=buf)
+        assert q.is_contiguous()
+        outs.append((q, c.k, c.v, c.bounds))
+    for other in outs[1:]:
+        assert all(torch.equal(a, b) for a, b in zip(outs[0], other))
+    with pytest.raises(ValueError):
+        B.paged_append(p, g, qkv[:, 8:10], qkv[:, 9:10])
+    with pytest.raises(TypeError):
+        B.paged_append(p, g, qkv[:, 8:10].float(), qkv[:, 10:])
+
+
+def test_a_graph_whose_sequences_grow_over_the_rows_of_one_launch():
+    """A captured attention replayed with other lengths, from none to the table's, on either side of every rule that the host cannot see."""
+    for max_pages, page in ((20, 16), (300, 64)):                 # one launch; shares
+        p = _params(8, 2, 128, BF16)
+        full = max_pages * page
+        c = Cache([full] * 3, 2, 128, page, BF16, seed=max_pages, bounds=True, max_pages=max_pages).fill()
+        g = c.handle(p)
+        q = c.randn(3, 8, 128)
+        side = torch.cuda.Stream()
+        side.wait_stream(torch.cuda.current_stream())
+        with torch.cuda.stream(side):
+            B.paged_attention(p, g, q, want_lse=True)
+        torch.cuda.current_stream().wait_stream(side)
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            out, lse = B.paged_attention(p, g, q, want_lse=True)
+            sparse, sel = B.paged_sparse_attention(p, g, q, 6)
+        for lens in ([0, 0, 0], [1, 0, full], [full - 1, 17, page * 6], [page * 6 + 1, 5, 64]):
+            c.lens.copy_(torch.tensor(lens))
+            for pages in range(3):
+                c.set_bounds(pages, lens[pages])
+            graph.replay()
+            ref, ref_lse = R.attention(c, q)
+            assert float((out.double() - ref).abs().max()) <= 2e-5 * 6
+            want = [[R.choose(x, 6, 1, 1) for x in heads] for heads in R.scores(c, q)]
+            assert sel.tolist() == [[x + [-1] * (6 - len(x)) for x in heads] for heads in want]
+            assert float((sparse.double() - R.attention(c, q, want)[0]).abs().max()) <= 2e-5 * 6
