@@ -355,7 +355,7 @@ sablock_status_t sablock_paged_attention(const sablock_params_t *p, const sabloc
  * in double, rounded once to fp32; ties go to the lower page.  The first n_first and the last n_last pages of a sequence are always
  * in (n_first + n_last <= n_selected).  A score that is no number ranks above all others, a page that is not followed below.
  *  selected dev int32 [n_seqs, Hkv, n_selected]: page indices, ascending; all pages and then -1 where there are not more.
- * max_pages at most 49152. */
+ * max_pages at most 49152, n_seqs * n_kv_heads at most 65535, n_selected * page_size at most 2^30. */
 sablock_status_t sablock_page_select(const sablock_params_t *p, const sablock_pages_t *pages, const void *q,
                                      int n_selected, int n_first, int n_last, int *selected,
                                      sablock_stream_t stream);

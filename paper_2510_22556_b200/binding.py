@@ -463,6 +463,7 @@ def make_pages(p: Params, k_pages: torch.Tensor, v_pages: torch.Tensor, table: t
     if bounds is not None:
         g.bounds = _contiguous("bounds", bounds, dt, dev, (g.n_pages, hkv, 2, d))
     g._refs = k_pages, v_pages, table, seq_lens, bounds
+    g._block, g._sizes = p, (p.n_q_heads, p.n_kv_heads, p.head_dim, p.dtype)
     g._dtype, g._device, g._index, g._q_shape = dt, dev, -1 if dev.index is None else dev.index, (g.n_seqs, p.n_q_heads, d)
     # what the calls' outputs and scratch look like: empty_like of a tensor costs half of an empty
     g._lse_like = torch.empty(1, device=dev).expand(g.n_seqs, p.n_q_heads)
@@ -480,8 +481,11 @@ def paged_workspace_bytes(p: Params, pages: Pages, n_selected: int = -1) -> int:
     return n
 
 
-def _pages_stream(pages: Pages) -> int:
-    """torch's current stream; the current device has to be the cache's (a launch goes to the current one)."""
+def _pages_stream(p: Params, pages: Pages) -> int:
+    """torch's current stream; the parameter block has to be that of the cache and the current device the cache's (a launch goes
+    to the current one)."""
+    if p is not pages._block and (p.n_q_heads, p.n_kv_heads, p.head_dim, p.dtype) != pages._sizes:
+        raise ValueError("the parameter block is of other sizes than the one that the cache was described with")
     dev = torch._C._cuda_getDevice()
     if dev != pages._index:
         raise ValueError(f"the cache is on {pages._device}, the current device is cuda:{dev}")
@@ -506,7 +510,7 @@ def paged_append(p: Params, pages: Pages, k: torch.Tensor, v: torch.Tensor, q: O
     each), keys and queries q [n, H, D] rotated by positions * inv_freq on the way.  Returns the rotated queries."""
     l, fast = lib(), pages._fast
     if l.append_step is not None and fast is not None:
-        done = l.append_step(C.addressof(p), C.addressof(pages), fast, k, v, q, q_out, positions, inv_freq, interleaved, cu_new, _pages_stream(pages))
+        done = l.append_step(C.addressof(p), C.addressof(pages), fast, k, v, q, q_out, positions, inv_freq, interleaved, cu_new, _pages_stream(p, pages))
         if done is None or type(done) is torch.Tensor:
             return done
         if type(done) is int:
@@ -531,7 +535,7 @@ def paged_append(p: Params, pages: Pages, k: torch.Tensor, v: torch.Tensor, q: O
         freq_at = _contiguous("inv_freq", inv_freq, torch.float32, dev, (rotary // 2,))
     cu_at = None if cu_new is None else _contiguous("cu_new", cu_new, torch.int32, dev, (pages.n_seqs + 1,))
     code = l.paged_append(C.addressof(p), C.addressof(pages), n, cu_at, k.data_ptr(), ks, v.data_ptr(), vs, q_at, qs, out_at, pos_at,
-                              freq_at, rotary, 1 if interleaved else 0, _pages_stream(pages))
+                              freq_at, rotary, 1 if interleaved else 0, _pages_stream(p, pages))
     if code != OK:
         raise SablockError(code, "sablock_paged_append")
     return q_out
@@ -552,7 +556,7 @@ def paged_attention(p: Params, pages: Pages, q: torch.Tensor, selected: Optional
         like = _like(p, pages, 0 if selected is None else -1)[0]
         ws = None if like is None else torch.empty_like(like)
     code = lib().paged_attention(C.addressof(p), C.addressof(pages), q_at, sel_at, n, out.data_ptr(), lse.data_ptr() if want_lse else None,
-                                 None if ws is None else ws.data_ptr(), 0 if ws is None else ws.numel(), _pages_stream(pages))
+                                 None if ws is None else ws.data_ptr(), 0 if ws is None else ws.numel(), _pages_stream(p, pages))
     if code != OK:
         raise SablockError(code, "sablock_paged_attention")
     return (out, lse) if want_lse else out
@@ -562,7 +566,7 @@ def page_select(p: Params, pages: Pages, q: torch.Tensor, n_selected: int, n_fir
     """The pages whose bounds promise the largest logits, per KV head: int32 [n_seqs, Hkv, n_selected], ascending, then -1."""
     q_at = _contiguous("q", q, pages._dtype, pages._device, pages._q_shape)
     selected = torch.empty_like(_like(p, pages, n_selected)[1])
-    _check(lib().page_select(C.addressof(p), C.addressof(pages), q_at, n_selected, n_first, n_last, _ptr(selected), _pages_stream(pages)),
+    _check(lib().page_select(C.addressof(p), C.addressof(pages), q_at, n_selected, n_first, n_last, _ptr(selected), _pages_stream(p, pages)),
            "sablock_page_select")
     return selected
 
@@ -579,7 +583,7 @@ def paged_sparse_attention(p: Params, pages: Pages, q: torch.Tensor, n_selected:
         ws = torch.empty_like(ws_like)
     code = lib().paged_sparse_attention(C.addressof(p), C.addressof(pages), q_at, n_selected, n_first, n_last, selected.data_ptr(),
                                         out.data_ptr(), lse.data_ptr() if want_lse else None, None if ws is None else ws.data_ptr(),
-                                        0 if ws is None else ws.numel(), _pages_stream(pages))
+                                        0 if ws is None else ws.numel(), _pages_stream(p, pages))
     if code != OK:
         raise SablockError(code, "sablock_paged_sparse_attention")
     return (out, selected, lse) if want_lse else (out, selected)

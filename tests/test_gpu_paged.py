@@ -476,6 +476,75 @@ def test_a_cache_on_another_device_than_the_current_one_is_refused():
             call()
 
 
+def test_another_parameter_block_than_the_caches():
+    p = _params(4, 2, 16, F32)
+    c = Cache([5], 2, 16, 4, F32, bounds=True).fill()
+    g = c.handle(p)
+    x, q = c.randn(1, 2, 16), c.randn(1, 4, 16)
+    same, others = _params(4, 2, 16, F32), [_params(8, 2, 16, F32), _params(4, 4, 16, F32), _params(4, 2, 32, F32), _params(4, 2, 16, BF16)]
+    assert torch.equal(B.paged_attention(p, g, q), B.paged_attention(same, g, q))
+    for o in others:
+        for call in (lambda: B.paged_append(o, g, x, x), lambda: B.paged_attention(o, g, q), lambda: B.page_select(o, g, q, 2),
+                     lambda: B.paged_sparse_attention(o, g, q, 2)):
+            with pytest.raises((ValueError, TypeError)):
+                call()
+
+
+def test_as_many_sequences_as_a_call_takes():
+    n = 4096
+    p = _params(2, 1, 64, BF16)
+    lens = [(i * 5) % 23 for i in range(n)]
+    c = Cache(lens, 1, 64, 8, BF16, fill=0.0, bounds=True)
+    new = [min(x, i % 4) for i, x in enumerate(lens)]
+    for s, x in enumerate(lens):
+        at = c.rows(s, x - new[s])
+        c.k[at], c.v[at] = c.randn(x - new[s], 1, 64), c.randn(x - new[s], 1, 64)
+        c.set_bounds(s, x - new[s])
+    k, v = c.randn(sum(new), 1, 64), c.randn(sum(new), 1, 64)
+    g = c.handle(p)
+    B.paged_append(p, g, k, v, cu_new=torch.tensor([0] + new, device="cuda").cumsum(0).to(torch.int32))
+    kept, t = c.bounds.clone(), 0
+    for s, x in enumerate(lens):
+        for r in range(x - new[s], x):
+            assert torch.equal(c.k[c.place(s, r)], k[t]) and torch.equal(c.v[c.place(s, r)], v[t])
+            t += 1
+        if new[s]:
+            c.set_bounds(s, x)
+    assert torch.equal(kept, c.bounds)
+    q = c.randn(n, 2, 64)
+    _check_attention(c, p, q)
+    want = [[R.choose(x, 2, 0, 1) for x in heads] for heads in R.scores(c, q)]
+    sel = B.page_select(p, g, q, 2, 0, 1)
+    assert sel.tolist() == [[x + [-1] * (2 - len(x)) for x in heads] for heads in want]
+    _check_attention(c, p, q, sel, want)
+
+
+def test_one_page_per_sequence():
+    """A cache of long rows that are not split at all: the page is the sequence."""
+    p = _params(4, 2, 64, BF16)
+    c = Cache([0, 0], 2, 64, 3000, BF16, bounds=True, max_pages=1, spare=0)
+    g = c.handle(p)
+    new = [2500, 130]
+    for part in (0.5, 1.0):                                  # in two parts: the second widens the bounds of the first
+        had = c.lens.tolist()
+        c.lens.copy_(torch.tensor([int(x * part) for x in new]))
+        n = [a - b for a, b in zip(c.lens.tolist(), had)]
+        k, v = c.randn(sum(n), 2, 64), c.randn(sum(n), 2, 64)
+        B.paged_append(p, g, k, v, cu_new=torch.tensor([0] + n, device="cuda").cumsum(0).to(torch.int32))
+        t = 0
+        for s in range(2):
+            page = int(c.table[s, 0])
+            assert torch.equal(c.k[page, had[s]:had[s] + n[s]], k[t:t + n[s]]) and torch.equal(c.v[page, had[s]:had[s] + n[s]], v[t:t + n[s]])
+            t += n[s]
+        got = c.bounds.clone()
+        for s in range(2):
+            c.set_bounds(s, c.lens.tolist()[s])
+        assert torch.equal(got, c.bounds)
+    q = c.randn(2, 4, 64)
+    _check_attention(c, p, q)
+    assert B.page_select(p, g, q, 3).tolist() == [[[0, -1, -1]] * 2] * 2
+
+
 def test_append_through_ctypes_and_through_the_module():
     """The binding without its marshalling module, and a caller's own buffer for the queries, do the same."""
     p = _params(8, 2, 64, BF16)
