@@ -416,8 +416,8 @@ def _token_stride(t: torch.Tensor, dtype: torch.dtype, device, n: int, heads: in
     """Elements from token to token of a [n, heads, d] tensor whose heads are contiguous, -1 where it is none."""
     if t.dtype != dtype or t.device != device or t.shape != (n, heads, d):
         return -1
-    if n and ((d > 1 and t.stride(2) != 1) or (heads > 1 and t.stride(1) != d)):
-        return -1
+    if n and ((d > 1 and t.stride(2) != 1) or (heads > 1 and t.stride(1) != d) or (n > 1 and t.stride(0) == 0)):
+        return -1                                  # (one token repeated: to the entry points a stride of 0 says contiguous)
     return t.stride(0) if n > 1 else 0
 
 
@@ -436,7 +436,7 @@ def _tokens(name: str, t: torch.Tensor, dtype: torch.dtype, device, n: int, head
     """Token stride of a [n, heads, d] tensor whose heads are contiguous; refuses others."""
     s = _token_stride(t, dtype, device, n, heads, d) if isinstance(t, torch.Tensor) else -1
     if s < 0:
-        _refuse(name, t, dtype, device, (n, heads, d), "the heads of a token must be contiguous")
+        _refuse(name, t, dtype, device, (n, heads, d), "the heads of a token must be contiguous, and tokens lie apart")
     return s
 
 
@@ -449,8 +449,12 @@ def make_pages(p: Params, k_pages: torch.Tensor, v_pages: torch.Tensor, table: t
     for name, t, shape in (("k_pages", k_pages, (None, None, hkv, d)), ("v_pages", v_pages, (*k_pages.shape[:2], hkv, d))):
         if t.dtype != dt or t.device != dev or t.dim() != 4 or t.shape[2:] != (hkv, d) or t.shape != k_pages.shape or (d > 1 and t.stride(3) != 1):
             _refuse(name, t, dt, dev, shape, "channels must be contiguous")
+        if any(t.stride(i) == 0 and t.shape[i] > 1 for i in range(3)):
+            raise ValueError(f"{name}: pages, rows and heads must lie apart")       # (to the entry points a stride of 0 says contiguous)
     if table.dtype != torch.int32 or table.device != dev or table.dim() != 2 or (table.shape[1] > 1 and table.stride(1) != 1):
         _refuse("table", table, torch.int32, dev, (None, None), "the entries of a sequence must be contiguous")
+    if table.shape[0] > 1 and table.stride(0) < table.shape[1]:
+        raise ValueError("table: the sequences' entries must lie apart")
     g = Pages()
     for name, t in (("k", k_pages), ("v", v_pages)):
         setattr(g, name, t.data_ptr())

@@ -149,7 +149,8 @@ static PyObject* bind_decode(PyObject* module, PyObject* address)
 
 /* What the calls over a paged cache check of a tensor, a few attributes each, in a third of the time that the same takes in
  * Python.  fits(tensor, dtype, device, shape): whether it is that and contiguous; token_stride(tensor, dtype, device, n, heads, channels):
- * elements from token to token of a tensor [n, heads, channels] whose heads are contiguous (0 where n < 2), -1 where it is none. */
+ * elements from token to token of a tensor [n, heads, channels] whose heads are contiguous (0 where n < 2), -1 where it is none (nor is one
+ * token repeated: a stride of 0 says contiguous). */
 static PyObject *s_dtype, *s_device, *s_contiguous, *s_stride;
 
 /* 1: attribute `name` of t equals v; 0: it does not; -1: an error. */
@@ -227,7 +228,7 @@ static long long stride_of(PyObject* t, PyObject* dtype, PyObject* device, long 
         Py_DECREF(x);
     }
     if (rc < 0) return -2;
-    if (rc == 1 && n > 0) rc = (d < 2 || stride[2] == 1) && (heads < 2 || stride[1] == d);
+    if (rc == 1 && n > 0) rc = (d < 2 || stride[2] == 1) && (heads < 2 || stride[1] == d) && (n < 2 || stride[0] > 0);
     return rc != 1 ? -1 : n > 1 ? stride[0] : 0;
 }
 

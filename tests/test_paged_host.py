@@ -149,6 +149,8 @@ def test_make_pages_refuses(lib):
     k, v, table, lens = _tensors()
     for bad in [(k.bfloat16(), v, table, lens), (k, v[:5], table, lens), (k, v, table.long(), lens), (k, v, table, lens[:1]), (k[0], v[0], table, lens),
                 (k.flip(3).transpose(2, 3).contiguous().transpose(2, 3), v, table, lens), (k, v, table.t().contiguous().t(), lens),
+                (k[:1].expand(6, -1, -1, -1), v, table, lens), (k, v[:, :, :1].expand(-1, -1, 2, -1), table, lens), (k, v[:, :1].expand(-1, 4, -1, -1), table, lens),
+                (k, v, table[:1].expand(2, -1), lens), (k, v, torch.zeros(9, dtype=torch.int32).as_strided((2, 3), (1, 1)), lens),
                 (k, v, table, lens, torch.zeros(6, 2, 16)), (k, v, table, lens, torch.zeros(6, 2, 2, 32)[..., ::2])]:
         with pytest.raises((TypeError, ValueError)):
             B.make_pages(p, *bad)
@@ -161,7 +163,7 @@ def test_calls_refuse_tensors_that_do_not_fit(lib):
     pos, freq = torch.zeros(2, dtype=torch.int32), torch.zeros(8)
     for a, kw in [((x[:1], x), {}), ((x.half(), x), {}), ((x, x), dict(q=q[:, :3])), ((x, x), dict(q=q.transpose(1, 2).contiguous().transpose(1, 2))),
                   ((x, x), dict(q_out=q)), ((x, x), dict(q=q, q_out=q[:1])), ((x, x), dict(positions=pos.long())), ((x, x), dict(positions=pos[:1])),
-                  ((x, x), dict(inv_freq=freq.double())), ((x, x), dict(cu_new=pos)), ((x, x), dict(inv_freq=torch.zeros(16)[::2]))]:
+                  ((x[:1].expand(2, -1, -1), x), {}), ((x, x), dict(q=q[:1].expand(2, -1, -1))), ((x, x), dict(inv_freq=freq.double())), ((x, x), dict(cu_new=pos)), ((x, x), dict(inv_freq=torch.zeros(16)[::2]))]:
         with pytest.raises((TypeError, ValueError)):
             B.paged_append(p, g, *a, **kw)
     for fn in (lambda t: B.paged_attention(p, g, t), lambda t: B.page_select(p, g, t, 2), lambda t: B.paged_sparse_attention(p, g, t, 2)):
@@ -185,7 +187,7 @@ def test_tensor_checks_of_the_marshalling_module(n, heads, d):
     for t in views:
         slow = -1
         if t.dtype == torch.float32 and t.device == cpu and t.shape == (n, heads, d) and \
-                not (n and ((d > 1 and t.stride(2) != 1) or (heads > 1 and t.stride(1) != d))):
+                not (n and ((d > 1 and t.stride(2) != 1) or (heads > 1 and t.stride(1) != d) or (n > 1 and t.stride(0) == 0))):
             slow = t.stride(0) if n > 1 else 0
         got.append(fast.token_stride(t, torch.float32, cpu, n, heads, d))
         assert got[-1] == slow
