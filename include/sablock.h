@@ -294,7 +294,8 @@ sablock_status_t sablock_decode_attention(const sablock_params_t *p, int n_prob,
  * number of query heads per KV head, any page size.  Up to 4096 sequences of up to 2^30 rows.
  * Device data that says what cannot be stays inside the buffers: lengths are taken as at least 0 and at most
  * max_pages * page_size, and a page number outside [0, n_pages) is not followed (append drops the row, attention treats it as
- * absent).  Two rows of one append that fall on the same place (a page that is in two tables) leave either's values. */
+ * absent).  Two rows of one append that fall on the same place (a page that is in two tables) leave either's values.  The device arrays
+ * must not change while a call that reads them runs (as with every call here: calls on one stream follow one another). */
 typedef struct sablock_pages {
     void *k, *v;                   /* dev pools [n_pages, page_size, Hkv, D] through the strides        */
     void *bounds;                  /* dev [n_pages, Hkv, 2, D] (dtype of the block) or NULL: the smallest and the
@@ -353,7 +354,8 @@ sablock_status_t sablock_paged_attention(const sablock_params_t *p, const sabloc
 /* Which pages a token's queries should look at: for each KV head the n_selected pages whose bounds (required) promise the largest logits,
  *   score(page) = sum over the head's queries h and channels d of max(q[h][d] * lo[d], q[h][d] * hi[d]),
  * in double, rounded once to fp32; ties go to the lower page.  The first n_first and the last n_last pages of a sequence are always
- * in (n_first + n_last <= n_selected).  A score that is no number ranks above all others, a page that is not followed below.
+ * in (n_first + n_last <= n_selected).  A page with a bound that is not finite ranks above all that have none, one that is not
+ * followed below.
  *  selected dev int32 [n_seqs, Hkv, n_selected]: page indices, ascending; all pages and then -1 where there are not more.
  * max_pages at most 49152, n_seqs * n_kv_heads at most 65535, n_selected * page_size at most 2^30. */
 sablock_status_t sablock_page_select(const sablock_params_t *p, const sablock_pages_t *pages, const void *q,

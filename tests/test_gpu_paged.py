@@ -291,6 +291,23 @@ def test_page_select_ties_infinities_and_missing_numbers():
     assert sorted(set(range(300)) - set(chosen)) == [250]
 
 
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("H", [1, 4])
+def test_page_select_infinite_bounds(dtype, H):
+    """Whatever the signs of the queries, a page with an infinite bound comes in before those without, through either call."""
+    p = _params(H, 1, 32, dtype)
+    for seed, (side, x) in enumerate([(0, -math.inf), (1, math.inf), (0, math.inf), (1, -math.inf)]):
+        c = Cache([8 * 90], 1, 32, 8, dtype, seed=seed, bounds=True).fill()
+        q = c.randn(1, H, 32)
+        q[0, 0, 7] = 0.0
+        for page, channel in ((33, 7), (61, 4), (62, 30)):
+            c.bounds[int(c.table[0, page]), 0, side, channel] = x
+            if x * (1 if side else -1) < 0:                       # all keys of the channel are that
+                c.bounds[int(c.table[0, page]), 0, :, channel] = x
+        assert B.page_select(p, c.handle(p), q, 3, 0, 0).tolist() == [[[33, 61, 62]]]
+        assert B.paged_sparse_attention(p, c.handle(p), q, 3, 0, 0)[1].tolist() == [[[33, 61, 62]]]
+
+
 def test_page_select_many_pages():
     """As many pages as the kernel holds, with scores that are close together."""
     n = 49152
