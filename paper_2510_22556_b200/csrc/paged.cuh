@@ -357,6 +357,10 @@ __device__ __forceinline__ void append_bounds(const AppendArgs& a, const ApRun& 
         const int cols = min(kApThreads, c0 + n_cols - c), lanes = kApThreads / cols, tl = tid / cols, col = tid - tl * cols;
         const int h = (c + col) / PR, d = (c + col) % PR * E;
         const T* src = static_cast<const T*>(pg.k) + (long long)page * pg.k_page + (long long)at * pg.k_row + (long long)h * pg.k_head + d;
+        T* dst = static_cast<T*>(pg.bounds) + (((size_t)page * a.Hkv + h) * 2) * a.D + d;
+        uint4 *lo = reinterpret_cast<uint4*>(dst), *hi = reinterpret_cast<uint4*>(dst + a.D);
+        uint4 was_lo = {}, was_hi = {};              // what earlier rows left, asked for before the new rows
+        if (at > 0) { was_lo = *lo; was_hi = *hi; }
         constexpr uint32_t inf = ApBounds<T>::kInf, neg = ApBounds<T>::kNegInf;
         uint4 b[2] = {make_uint4(inf, inf, inf, inf), make_uint4(neg, neg, neg, neg)};
         if (tl < lanes)
@@ -372,9 +376,7 @@ __device__ __forceinline__ void append_bounds(const AppendArgs& a, const ApRun& 
         __syncthreads();
         if (tl == 0) {
             for (int l = 1; l < lanes; ++l) widen<T>(b, red[l * cols + col], red[kApThreads + l * cols + col]);
-            T* dst = static_cast<T*>(pg.bounds) + (((size_t)page * a.Hkv + h) * 2) * a.D + d;
-            uint4 *lo = reinterpret_cast<uint4*>(dst), *hi = reinterpret_cast<uint4*>(dst + a.D);
-            if (at > 0) widen<T>(b, *lo, *hi);
+            if (at > 0) widen<T>(b, was_lo, was_hi);
             *lo = b[0];
             *hi = b[1];
         }
