@@ -497,7 +497,8 @@ def _pages_stream(p: Params, pages: Pages) -> int:
 
 
 def _like(p: Params, pages: Pages, n_selected: int):
-    """What the scratch (None where a call needs none) and the page list of such a call look like."""
+    """What the scratch (None where a call needs none) and the page list of such a call look like; kept with the handle, so the block
+    has been found to be the cache's (_pages_stream) before."""
     like = pages._like.get(n_selected)
     if like is None:
         n, dev = paged_workspace_bytes(p, pages, n_selected), pages._device
@@ -554,13 +555,14 @@ def paged_attention(p: Params, pages: Pages, q: torch.Tensor, selected: Optional
     if selected is not None:
         n = selected.shape[-1]
         sel_at = _contiguous("selected", selected, torch.int32, pages._device, (pages.n_seqs, p.n_kv_heads, n))
+    stream = _pages_stream(p, pages)
     out = torch.empty_like(q, dtype=torch.float32)
     lse = torch.empty_like(pages._lse_like) if want_lse else None
     if ws is None:
         like = _like(p, pages, 0 if selected is None else -1)[0]
         ws = None if like is None else torch.empty_like(like)
     code = lib().paged_attention(C.addressof(p), C.addressof(pages), q_at, sel_at, n, out.data_ptr(), lse.data_ptr() if want_lse else None,
-                                 None if ws is None else ws.data_ptr(), 0 if ws is None else ws.numel(), _pages_stream(p, pages))
+                                 None if ws is None else ws.data_ptr(), 0 if ws is None else ws.numel(), stream)
     if code != OK:
         raise SablockError(code, "sablock_paged_attention")
     return (out, lse) if want_lse else out
@@ -569,8 +571,9 @@ def paged_attention(p: Params, pages: Pages, q: torch.Tensor, selected: Optional
 def page_select(p: Params, pages: Pages, q: torch.Tensor, n_selected: int, n_first: int = 1, n_last: int = 1) -> torch.Tensor:
     """The pages whose bounds promise the largest logits, per KV head: int32 [n_seqs, Hkv, n_selected], ascending, then -1."""
     q_at = _contiguous("q", q, pages._dtype, pages._device, pages._q_shape)
+    stream = _pages_stream(p, pages)
     selected = torch.empty_like(_like(p, pages, n_selected)[1])
-    _check(lib().page_select(C.addressof(p), C.addressof(pages), q_at, n_selected, n_first, n_last, _ptr(selected), _pages_stream(p, pages)),
+    _check(lib().page_select(C.addressof(p), C.addressof(pages), q_at, n_selected, n_first, n_last, _ptr(selected), stream),
            "sablock_page_select")
     return selected
 
@@ -579,6 +582,7 @@ def paged_sparse_attention(p: Params, pages: Pages, q: torch.Tensor, n_selected:
                            ws: Optional[torch.Tensor] = None, want_lse: bool = False):
     """page_select and paged_attention over what it selects.  Returns (out, selected), and lse behind them."""
     q_at = _contiguous("q", q, pages._dtype, pages._device, pages._q_shape)
+    stream = _pages_stream(p, pages)
     out = torch.empty_like(q, dtype=torch.float32)
     lse = torch.empty_like(pages._lse_like) if want_lse else None
     ws_like, sel_like = _like(p, pages, n_selected)
@@ -587,7 +591,7 @@ def paged_sparse_attention(p: Params, pages: Pages, q: torch.Tensor, n_selected:
         ws = torch.empty_like(ws_like)
     code = lib().paged_sparse_attention(C.addressof(p), C.addressof(pages), q_at, n_selected, n_first, n_last, selected.data_ptr(),
                                         out.data_ptr(), lse.data_ptr() if want_lse else None, None if ws is None else ws.data_ptr(),
-                                        0 if ws is None else ws.numel(), _pages_stream(p, pages))
+                                        0 if ws is None else ws.numel(), stream)
     if code != OK:
         raise SablockError(code, "sablock_paged_sparse_attention")
     return (out, selected, lse) if want_lse else (out, selected)

@@ -1,0 +1,36 @@
+"""Calls over a paged cache on the GPU after calls that were refused, and with tensors of unusual layouts."""
+import pytest
+import torch
+
+import paged_reference as R
+from paged_reference import Cache
+from paper_2510_22556_b200 import binding as B
+from paper_2510_22556_b200 import build as build_lib
+
+pytestmark = pytest.mark.gpu
+BF16, F32 = torch.bfloat16, torch.float32
+
+
+@pytest.fixture(scope="module", autouse=True)
+def _built():
+    build_lib()
+    B.lib()
+
+
+def _params(H, Hkv, D, dtype):
+    return B.make_params(H, Hkv, D, 1, dtype)
+
+
+def test_good_calls_after_refused_ones():
+    """A handle that calls with other parameter blocks were refused on does what one does that they were not."""
+    p = _params(8, 4, 64, F32)
+    c = Cache([3000, 500], 4, 64, 16, F32, bounds=True).fill()
+    g, fresh, q = c.handle(p), c.handle(p), c.randn(2, 8, 64)
+    for o in (_params(8, 2, 64, F32), _params(8, 4, 4, F32), _params(32, 4, 64, F32)):
+        for call in (lambda: B.paged_attention(o, g, q), lambda: B.page_select(o, g, q, 6), lambda: B.paged_sparse_attention(o, g, q, 6)):
+            with pytest.raises(ValueError):
+                call()
+    want = [[R.choose(x, 6, 1, 1) for x in heads] for heads in R.scores(c, q)]
+    assert B.page_select(p, g, q, 6).tolist() == want
+    assert torch.equal(B.paged_attention(p, g, q), B.paged_attention(p, fresh, q))
+    assert all(torch.equal(a, b) for a, b in zip(B.paged_sparse_attention(p, g, q, 6), B.paged_sparse_attention(p, fresh, q, 6)))

@@ -1,0 +1,46 @@
+"""What the binding's calls over a paged cache do with a call that they refuse, with blocks and tensors that change, with nothing to do:
+on the host (no GPU), the entry points themselves replaced where a good call would enqueue work."""
+import pytest
+import torch
+
+from paper_2510_22556_b200 import binding as B
+from paper_2510_22556_b200 import build as build_lib
+
+
+@pytest.fixture(scope="module", autouse=True)
+def _built():
+    build_lib()
+    B.lib()
+
+
+def _params(H=8, Hkv=4, D=16, dtype=torch.float32):
+    return B.make_params(H, Hkv, D, 1, dtype)
+
+
+def _cache(p, seqs=2, page=4, max_pages=3, n_pages=8):
+    """Handle of a small cache on the CPU."""
+    dt, hkv, d = {B.F32: torch.float32, B.BF16: torch.bfloat16}[p.dtype], p.n_kv_heads, p.head_dim
+    k, v = (torch.zeros(n_pages, page, hkv, d, dtype=dt) for _ in range(2))
+    return B.make_pages(p, k, v, torch.zeros(seqs, max_pages, dtype=torch.int32), torch.zeros(seqs, dtype=torch.int32), torch.zeros(n_pages, hkv, 2, d, dtype=dt))
+
+
+def _like(p, g, n):
+    """What a call allocates: bytes of scratch, shape of the page list."""
+    ws, sel = B._like(p, g, n)
+    return None if ws is None else ws.numel(), tuple(sel.shape)
+
+
+@pytest.mark.parametrize("why", ["heads", "kv_heads", "head_dim", "device"])
+def test_a_refused_call_leaves_the_handle_as_it_was(monkeypatch, why):
+    """The scratch and the page list of the next good call have the sizes that they have on a handle that no call was refused on."""
+    p = _params()
+    g, fresh, q = _cache(p), _cache(p), torch.zeros(2, 8, 16)
+    bad = {"heads": _params(H=32), "kv_heads": _params(Hkv=2), "head_dim": _params(D=4), "device": p}[why]
+    monkeypatch.setattr(torch._C, "_cuda_getDevice", lambda: 3, raising=False)
+    for call in (lambda: B.paged_attention(bad, g, q), lambda: B.paged_attention(bad, g, q, selected=torch.zeros(2, bad.n_kv_heads, 2, dtype=torch.int32)),
+                 lambda: B.page_select(bad, g, q, 2), lambda: B.paged_sparse_attention(bad, g, q, 2)):
+        with pytest.raises(ValueError):
+            call()
+    assert not g._like
+    for n in (0, -1, 2):
+        assert _like(p, g, n) == _like(p, fresh, n)
