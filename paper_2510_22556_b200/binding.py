@@ -444,7 +444,8 @@ def make_pages(p: Params, k_pages: torch.Tensor, v_pages: torch.Tensor, table: t
                bounds: Optional[torch.Tensor] = None) -> Pages:
     """Description of a paged cache: pools [n_pages, page_size, Hkv, D] (any strides with contiguous channels), table int32
     [n_seqs, max_pages], seq_lens int32 [n_seqs], bounds [n_pages, Hkv, 2, D] where pages are to be selected.  It refers to the
-    tensors: what they hold at the time of a call counts, and they live as long as it does."""
+    tensors: what they hold at the time of a call counts, and they live as long as it does.  Its own fields stay as they are: other
+    tensors or sizes are another description."""
     dt, dev, hkv, d = {F32: torch.float32, BF16: torch.bfloat16}[p.dtype], k_pages.device, p.n_kv_heads, p.head_dim
     for name, t, shape in (("k_pages", k_pages, (None, None, hkv, d)), ("v_pages", v_pages, (*k_pages.shape[:2], hkv, d))):
         if t.dtype != dt or t.device != dev or t.dim() != 4 or t.shape[2:] != (hkv, d) or t.shape != k_pages.shape or (d > 1 and t.stride(3) != 1):
@@ -467,7 +468,7 @@ def make_pages(p: Params, k_pages: torch.Tensor, v_pages: torch.Tensor, table: t
     if bounds is not None:
         g.bounds = _contiguous("bounds", bounds, dt, dev, (g.n_pages, hkv, 2, d))
     g._refs = k_pages, v_pages, table, seq_lens, bounds
-    g._block, g._sizes = p, (p.n_q_heads, p.n_kv_heads, p.head_dim, p.dtype)
+    g._sizes = (p.n_q_heads, p.n_kv_heads, p.head_dim, p.dtype)
     g._dtype, g._device, g._index, g._q_shape = dt, dev, -1 if dev.index is None else dev.index, (g.n_seqs, p.n_q_heads, d)
     # what the calls' outputs and scratch look like: empty_like of a tensor costs half of an empty
     g._lse_like = torch.empty(1, device=dev).expand(g.n_seqs, p.n_q_heads)
@@ -488,7 +489,7 @@ def paged_workspace_bytes(p: Params, pages: Pages, n_selected: int = -1) -> int:
 def _pages_stream(p: Params, pages: Pages) -> int:
     """torch's current stream; the parameter block has to be that of the cache and the current device the cache's (a launch goes
     to the current one)."""
-    if p is not pages._block and (p.n_q_heads, p.n_kv_heads, p.head_dim, p.dtype) != pages._sizes:
+    if (p.n_q_heads, p.n_kv_heads, p.head_dim, p.dtype) != pages._sizes:         # (the cache's own block too: its fields may have changed)
         raise ValueError("the parameter block is of other sizes than the one that the cache was described with")
     dev = torch._C._cuda_getDevice()
     if dev != pages._index:

@@ -44,3 +44,17 @@ def test_a_refused_call_leaves_the_handle_as_it_was(monkeypatch, why):
     assert not g._like
     for n in (0, -1, 2):
         assert _like(p, g, n) == _like(p, fresh, n)
+
+
+@pytest.mark.parametrize("field,value", [("n_q_heads", 16), ("n_kv_heads", 2), ("head_dim", 32), ("dtype", B.BF16)])
+def test_a_block_whose_sizes_changed_after_the_cache_was_described(field, value):
+    """The block is the caller's to change; with other sizes than the cache's it is refused though it is the same block."""
+    p = _params()
+    g = _cache(p)
+    setattr(p, field, value)
+    q, x, sel = torch.zeros(2, 8, 16), torch.zeros(2, p.n_kv_heads, p.head_dim), torch.zeros(2, p.n_kv_heads, 2, dtype=torch.int32)
+    for call in (lambda: B.paged_append(p, g, x, x), lambda: B.paged_attention(p, g, q), lambda: B.paged_attention(p, g, q, selected=sel),
+                 lambda: B.page_select(p, g, q, 2), lambda: B.paged_sparse_attention(p, g, q, 2)):
+        with pytest.raises(ValueError, match="other sizes"):
+            call()
+    assert not g._like
