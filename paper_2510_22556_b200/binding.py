@@ -432,6 +432,17 @@ def _contiguous(name: str, t: torch.Tensor, dtype: torch.dtype, device, shape) -
     return t.data_ptr()
 
 
+def _scratch(pages: Pages, ws: Optional[torch.Tensor]):
+    """Address and bytes of a caller's scratch (one without a storage of that size, or elsewhere, is refused), none for None."""
+    if ws is None:
+        return None, 0
+    if not isinstance(ws, torch.Tensor):
+        raise TypeError(f"ws: a tensor expected, got {type(ws).__name__}")
+    if ws.device != pages._device or not ws.is_contiguous():
+        raise ValueError(f"ws: a contiguous tensor on {pages._device} expected")
+    return ws.data_ptr(), ws.numel()
+
+
 def _tokens(name: str, t: torch.Tensor, dtype: torch.dtype, device, n: int, heads: int, d: int) -> int:
     """Token stride of a [n, heads, d] tensor whose heads are contiguous; refuses others."""
     s = _token_stride(t, dtype, device, n, heads, d) if isinstance(t, torch.Tensor) else -1
@@ -562,8 +573,9 @@ def paged_attention(p: Params, pages: Pages, q: torch.Tensor, selected: Optional
     if ws is None:
         like = _like(p, pages, 0 if selected is None else -1)[0]
         ws = None if like is None else torch.empty_like(like)
+    ws_at, ws_bytes = _scratch(pages, ws)
     code = lib().paged_attention(C.addressof(p), C.addressof(pages), q_at, sel_at, n, out.data_ptr(), lse.data_ptr() if want_lse else None,
-                                 None if ws is None else ws.data_ptr(), 0 if ws is None else ws.numel(), stream)
+                                 ws_at, ws_bytes, stream)
     if code != OK:
         raise SablockError(code, "sablock_paged_attention")
     return (out, lse) if want_lse else out
@@ -590,9 +602,9 @@ def paged_sparse_attention(p: Params, pages: Pages, q: torch.Tensor, n_selected:
     selected = torch.empty_like(sel_like)
     if ws is None and ws_like is not None:
         ws = torch.empty_like(ws_like)
+    ws_at, ws_bytes = _scratch(pages, ws)
     code = lib().paged_sparse_attention(C.addressof(p), C.addressof(pages), q_at, n_selected, n_first, n_last, selected.data_ptr(),
-                                        out.data_ptr(), lse.data_ptr() if want_lse else None, None if ws is None else ws.data_ptr(),
-                                        0 if ws is None else ws.numel(), stream)
+                                        out.data_ptr(), lse.data_ptr() if want_lse else None, ws_at, ws_bytes, stream)
     if code != OK:
         raise SablockError(code, "sablock_paged_sparse_attention")
     return (out, selected, lse) if want_lse else (out, selected)

@@ -58,3 +58,42 @@ def test_a_block_whose_sizes_changed_after_the_cache_was_described(field, value)
         with pytest.raises(ValueError, match="other sizes"):
             call()
     assert not g._like
+
+
+class _Entry:
+    """Stands in for the library: notes the arguments of the entry points that enqueue work, and enqueues nothing."""
+
+    def __init__(self, real):
+        self.real, self.calls = real, []
+
+    def __getattr__(self, name):
+        if name in ("paged_append", "paged_attention", "page_select", "paged_sparse_attention"):
+            return lambda *a: self.calls.append((name, a)) or 0
+        return getattr(self.real, name)
+
+
+@pytest.fixture
+def entry(monkeypatch):
+    """Good calls on CPU tensors go through the binding and end there."""
+    e = _Entry(B.lib())
+    monkeypatch.setattr(B, "lib", lambda: e)
+    monkeypatch.setattr(torch._C, "_cuda_getDevice", lambda: -1, raising=False)
+    monkeypatch.setattr(torch._C, "_cuda_getCurrentRawStream", lambda dev: 0, raising=False)
+    return e
+
+
+def test_scratch_that_is_not_what_its_size_says_is_refused(entry):
+    """Scratch on another device, or one element expanded, has an address and a number of elements that the entry points would believe."""
+    p = _params()
+    g, q = _cache(p), torch.zeros(2, 8, 16)
+    n = B.paged_workspace_bytes(p, g)
+    calls = (lambda ws: B.paged_attention(p, g, q, ws=ws), lambda ws: B.paged_sparse_attention(p, g, q, 2, ws=ws))
+    for ws in (torch.zeros(1, dtype=torch.uint8).expand(n), torch.zeros(2 * n, dtype=torch.uint8)[::2], torch.empty(n, dtype=torch.uint8, device="meta"), bytearray(n)):
+        for call in calls:
+            with pytest.raises((TypeError, ValueError)):
+                call(ws)
+    assert not entry.calls
+    ws = torch.zeros(n, dtype=torch.uint8)
+    for call in calls:
+        call(ws)
+    assert [a[-3:] for _, a in entry.calls] == [(ws.data_ptr(), n, 0)] * 2
