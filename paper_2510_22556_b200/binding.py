@@ -567,6 +567,8 @@ def paged_attention(p: Params, pages: Pages, q: torch.Tensor, selected: Optional
     if selected is not None:
         n = selected.shape[-1]
         sel_at = _contiguous("selected", selected, torch.int32, pages._device, (pages.n_seqs, p.n_kv_heads, n))
+        if n == 0:                                 # (without an address it would say all rows)
+            raise SablockError(1, "sablock_paged_attention")
     stream = _pages_stream(p, pages)
     out = torch.empty_like(q, dtype=torch.float32)
     lse = torch.empty_like(pages._lse_like) if want_lse else None

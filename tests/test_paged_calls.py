@@ -97,3 +97,17 @@ def test_scratch_that_is_not_what_its_size_says_is_refused(entry):
     for call in calls:
         call(ws)
     assert [a[-3:] for _, a in entry.calls] == [(ws.data_ptr(), n, 0)] * 2
+
+
+def test_an_empty_list_of_pages_is_not_all_of_them(entry):
+    """A list without entries has no address, which to the entry point says all rows."""
+    p = _params()
+    g, q = _cache(p), torch.zeros(2, 8, 16)
+    for sel in (torch.zeros(2, 4, 0, dtype=torch.int32), torch.zeros(2, 4, 3, dtype=torch.int32)[..., :0]):
+        with pytest.raises(B.SablockError) as e:
+            B.paged_attention(p, g, q, selected=sel)
+        assert e.value.code == 1
+    assert not entry.calls
+    sel = torch.zeros(2, 4, 1, dtype=torch.int32)
+    B.paged_attention(p, g, q, selected=sel)
+    assert entry.calls[0][1][3:5] == (sel.data_ptr(), 1)
