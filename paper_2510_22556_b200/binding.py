@@ -539,7 +539,7 @@ def paged_append(p: Params, pages: Pages, k: torch.Tensor, v: torch.Tensor, q: O
     if q is not None:
         qs, q_at = _tokens("q", q, dt, dev, n, H, d), q.data_ptr()
         if q_out is None:
-            q_out = torch.empty_like(q)            # (contiguous: tokens that do not lie side by side are not kept apart)
+            q_out = torch.empty_like(q, memory_format=torch.contiguous_format)
             out_at = q_out.data_ptr()
         else:
             out_at = _contiguous("q_out", q_out, dt, dev, (n, H, d))

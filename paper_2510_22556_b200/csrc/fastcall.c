@@ -276,6 +276,7 @@ static PyObject* invoke_append(PyObject* self, PyObject* const* args, Py_ssize_t
     int rc = (ks = stride_of(args[3], dtype, device, (long long)n, hkv, d)) >= 0 && (vs = stride_of(args[4], dtype, device, (long long)n, hkv, d)) >= 0;
     if (rc && has_q) rc = (qs = stride_of(args[5], dtype, device, (long long)n, heads, d)) >= 0;
     if (rc && !made) rc = args[6] == Py_None;        /* (a caller's own buffer takes the other way) */
+    if (rc && made) rc = qs == 0 || qs >= heads * d; /* (so do tokens that overlap: what looks like them would not be contiguous) */
     if (rc && args[7] != Py_None) rc = fits_vector(args[7], i32, device, (long long)n) == 1;
     if (rc && args[8] != Py_None) {
         rc = fits_vector(args[8], f32, device, -1) == 1 && take_extent(args[8], 1, 0, &rotary) == 0;

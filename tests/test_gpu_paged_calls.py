@@ -34,3 +34,15 @@ def test_good_calls_after_refused_ones():
     assert B.page_select(p, g, q, 6).tolist() == want
     assert torch.equal(B.paged_attention(p, g, q), B.paged_attention(p, fresh, q))
     assert all(torch.equal(a, b) for a, b in zip(B.paged_sparse_attention(p, g, q, 6), B.paged_sparse_attention(p, fresh, q, 6)))
+
+
+@pytest.mark.parametrize("stride", [16, 64, 128, 512, 1000])
+def test_append_with_queries_that_overlap(stride):
+    """Query tokens that lie closer than their heads are many (a window that slides) are read as they lie and come back token after token."""
+    p, n = _params(8, 2, 64, F32), 7
+    c = Cache([4, 3], 2, 64, 16, F32, fill=0.0)
+    q = c.randn(n * 1000 + 512).as_strided((n, 8, 64), (stride, 64, 1))
+    x, pos = c.randn(n, 2, 64), torch.arange(n, dtype=torch.int32, device="cuda") * 11
+    freq, cu = torch.linspace(1.0, 0.001, 32, device="cuda"), torch.tensor([0, 4, 7], dtype=torch.int32, device="cuda")
+    got = [B.paged_append(p, c.handle(p), x, x, q=t, positions=pos, inv_freq=freq, cu_new=cu) for t in (q, q.contiguous())]
+    assert got[0].is_contiguous() and torch.equal(*got)

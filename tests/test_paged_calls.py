@@ -1,5 +1,7 @@
 """What the binding's calls over a paged cache do with a call that they refuse, with blocks and tensors that change, with nothing to do:
 on the host (no GPU), the entry points themselves replaced where a good call would enqueue work."""
+import ctypes as C
+
 import pytest
 import torch
 
@@ -111,3 +113,34 @@ def test_an_empty_list_of_pages_is_not_all_of_them(entry):
     sel = torch.zeros(2, 4, 1, dtype=torch.int32)
     B.paged_attention(p, g, q, selected=sel)
     assert entry.calls[0][1][3:5] == (sel.data_ptr(), 1)
+
+
+@pytest.fixture
+def module(monkeypatch, entry):
+    """Appending goes through the marshalling module, CPU tensors too: the arguments of the entry point that it would call."""
+    fast = pytest.importorskip("paper_2510_22556_b200._fastcall")
+    got = []
+    fn = C.CFUNCTYPE(C.c_int, *[C.c_uint64] * 16)(lambda *a: got.append(a) or 0)
+    entry.append_step = fast.bind_append(C.cast(fn, C.c_void_p).value)
+    entry.keep = fn
+    return got
+
+
+def _module_handle(p, **kw):
+    g = _cache(p, **kw)
+    g._fast = g._dtype, g._device, g.n_seqs, p.n_kv_heads, p.n_q_heads, p.head_dim, torch.int32, torch.float32, torch.empty_like
+    return g
+
+
+@pytest.mark.parametrize("through_module", [False, True])
+@pytest.mark.parametrize("strides", [(8, 16, 1), (16, 16, 1), (48, 16, 1), (64, 16, 1), (120, 16, 1)])
+def test_the_rotated_queries_lie_side_by_side_whatever_the_queries_strides(module, entry, through_module, strides):
+    """Tokens that overlap (a stride below a token's heads) may be read, but what comes back is written token after token."""
+    p = _params(H=4, Hkv=1)
+    g = _module_handle(p, seqs=5) if through_module else _cache(p, seqs=5)
+    q, x = torch.zeros(1000).as_strided((5, 4, 16), strides), torch.zeros(5, 1, 16)
+    out = B.paged_append(p, g, x, x, q=q)
+    assert out.shape == q.shape and out.is_contiguous()
+    at = module[0] if module else entry.calls[0][1]
+    assert at[8:11] == (q.data_ptr(), strides[0], out.data_ptr())
+    assert len(module) + len(entry.calls) == 1 and bool(module) == (through_module and strides[0] >= 64)
