@@ -528,10 +528,10 @@ def paged_append(p: Params, pages: Pages, k: torch.Tensor, v: torch.Tensor, q: O
     l, fast = lib(), pages._fast
     if l.append_step is not None and fast is not None:
         done = l.append_step(C.addressof(p), C.addressof(pages), fast, k, v, q, q_out, positions, inv_freq, interleaved, cu_new, _pages_stream(p, pages))
-        if done is None or type(done) is torch.Tensor:
+        if done is not NotImplemented:
+            if type(done) is int:
+                raise SablockError(done, "sablock_paged_append")
             return done
-        if type(done) is int:
-            raise SablockError(done, "sablock_paged_append")
     # (something does not fit, or the module is not there: the same again, step by step)
     dt, dev, hkv, H, d = pages._dtype, pages._device, p.n_kv_heads, p.n_q_heads, p.head_dim
     n = k.shape[0]

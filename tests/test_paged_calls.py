@@ -144,3 +144,24 @@ def test_the_rotated_queries_lie_side_by_side_whatever_the_queries_strides(modul
     at = module[0] if module else entry.calls[0][1]
     assert at[8:11] == (q.data_ptr(), strides[0], out.data_ptr())
     assert len(module) + len(entry.calls) == 1 and bool(module) == (through_module and strides[0] >= 64)
+
+
+class _Named(torch.Tensor):
+    """A caller's own kind of tensor: what is made like it is of that kind too."""
+
+
+def test_an_append_of_another_kind_of_tensor_is_enqueued_once(module, entry):
+    p = _params(H=4, Hkv=1)
+    g, x, q = _module_handle(p, seqs=5), torch.zeros(5, 1, 16), torch.zeros(5, 4, 16).as_subclass(_Named)
+    out = B.paged_append(p, g, x, x, q=q)
+    assert len(module) == 1 and not entry.calls
+    assert out.shape == q.shape and out.data_ptr() == module[0][10]
+
+
+def test_a_status_of_the_module_is_raised_once(module, entry, monkeypatch):
+    p = _params(H=4, Hkv=1)
+    g, x = _module_handle(p, seqs=5), torch.zeros(5, 1, 16)
+    entry.append_step = lambda *a: module.append(a) or 4
+    with pytest.raises(B.SablockError) as e:
+        B.paged_append(p, g, x, x)
+    assert e.value.code == 4 and len(module) == 1 and not entry.calls
