@@ -318,7 +318,8 @@ size_t sablock_pages_sizeof(void);   /* sizeof(sablock_pages_t) as the library w
 /* Appends new tokens to their sequences, keys and queries rotated to their positions on the way.
  *  cu_new dev int32[n_seqs+1] or NULL: sequence s has the tokens [cu_new[s], cu_new[s+1]) of the arrays below, which become its last rows
  *  (the last of them row seq_lens[s] - 1); NULL: one token per sequence, n_tokens = n_seqs, and a sequence of length 0 (a padded
- *  batch) takes none.  Tokens behind cu_new[n_seqs] and tokens that have no place are left alone, their q_out too.
+ *  batch) takes none.  Tokens behind cu_new[n_seqs] and tokens that have no place are left alone, their q_out too.  n_tokens may be 0
+ *  with cu_new; k and v may then be NULL.
  *  k, v dev [n_tokens, Hkv, D], q dev [n_tokens, H, D] or NULL, heads contiguous, tokens k_stride, v_stride, q_stride elements apart (0 =
  *  contiguous; so the parts of one projection's output can be passed in); q_out dev [n_tokens, H, D] contiguous, not
  *  overlapping q; NULL with q.

@@ -1672,7 +1672,7 @@ sablock_status_t sablock_paged_append(const sablock_params_t* p, const sablock_p
     t_launches = 0;
     AppendArgs a;
     SAB_TRY(paged_args(p, pages, &a.pg));
-    if (!k || !v || !q != !q_out || n_tokens < 0 || k_stride < 0 || v_stride < 0 || q_stride < 0) return SABLOCK_ERR_INVALID_ARG;
+    if ((n_tokens && (!k || !v)) || !q != !q_out || n_tokens < 0 || k_stride < 0 || v_stride < 0 || q_stride < 0) return SABLOCK_ERR_INVALID_ARG;
     if (!cu_new && n_tokens != pages->n_seqs) return SABLOCK_ERR_INVALID_ARG;
     if (inv_freq ? rotary_dim < 2 || rotary_dim > p->head_dim || rotary_dim % 2 : rotary_dim != 0) return SABLOCK_ERR_INVALID_ARG;
     const int es = elem_size(p);

@@ -165,3 +165,21 @@ def test_a_status_of_the_module_is_raised_once(module, entry, monkeypatch):
     with pytest.raises(B.SablockError) as e:
         B.paged_append(p, g, x, x)
     assert e.value.code == 4 and len(module) == 1 and not entry.calls
+
+
+@pytest.mark.parametrize("through_module", [False, True])
+def test_appending_no_tokens(monkeypatch, through_module):
+    """A step in which no sequence has new tokens: tensors without elements have no address, and nothing is wrong with that."""
+    monkeypatch.setattr(torch._C, "_cuda_getDevice", lambda: -1, raising=False)
+    monkeypatch.setattr(torch._C, "_cuda_getCurrentRawStream", lambda dev: 0, raising=False)
+    p = _params(H=4, Hkv=1)
+    g = _module_handle(p) if through_module else _cache(p)
+    x, q, cu = torch.zeros(0, 1, 16), torch.zeros(0, 4, 16), torch.zeros(3, dtype=torch.int32)
+    pos, freq = torch.zeros(0, dtype=torch.int32), torch.ones(8)
+    assert B.paged_append(p, g, x, x, cu_new=cu) is None
+    out = B.paged_append(p, g, x, x, q=q, positions=pos, inv_freq=freq, cu_new=cu)
+    assert out.shape == (0, 4, 16) and B.last_launch_count() == 0
+    with pytest.raises(B.SablockError):            # one token each is not none
+        B.paged_append(p, g, x, x)
+    with pytest.raises(B.SablockError):
+        B.paged_append(p, g, x, x, cu_new=cu, inv_freq=torch.ones(9))
