@@ -321,8 +321,8 @@ size_t sablock_pages_sizeof(void);   /* sizeof(sablock_pages_t) as the library w
  *  batch) takes none.  Tokens behind cu_new[n_seqs] and tokens that have no place are left alone, their q_out too.  n_tokens may be 0
  *  with cu_new; k and v may then be NULL.
  *  k, v dev [n_tokens, Hkv, D], q dev [n_tokens, H, D] or NULL, heads contiguous, tokens k_stride, v_stride, q_stride elements apart (0 =
- *  contiguous; so the parts of one projection's output can be passed in); q_out dev [n_tokens, H, D] contiguous, not
- *  overlapping q; NULL with q.
+ *  contiguous; so the parts of one projection's output can be passed in); q_out dev [n_tokens, H, D] contiguous; NULL
+ *  with q.  q_out shares no byte with a token of q, k or v (SABLOCK_ERR_INVALID_ARG), nor with any other array of the call.
  *  k, v and q lie outside the pools.
  *  inv_freq dev f32[rotary_dim / 2], finite, or NULL (rotary_dim = 0: no rotation; how rows that the compression retained, which are
  *  rotated already, go into pages): the first rotary_dim channels of a head are turned in pairs (i, i + rotary_dim / 2), or

@@ -1080,6 +1080,13 @@ sablock_status_t launch_decode(const DecodeArgs& a, bool bf16, bool cluster, dim
 // ---- paged cache ---------------------------------------------------------------------------
 bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15) == 0; }
 
+// Whether the n_out bytes at `out` meet one of the n rows of `row` bytes that lie `step` > 0 bytes apart from `at` on.
+bool meets_rows(uintptr_t out, size_t n_out, uintptr_t at, size_t row, size_t step, size_t n)
+{
+    const size_t i = out < at + row ? 0 : (out - at - row) / step + 1;      // the first row that ends behind `out`
+    return i < n && at + i * step < out + n_out;
+}
+
 // The description of a paged cache, checked, as the kernels take it.  (Of the parameter block the heads, the head dimension and the type
 // count; the strides are the description's.)
 sablock_status_t paged_args(const sablock_params_t* p, const sablock_pages_t* pages, Paged* pg)
@@ -1423,7 +1430,8 @@ int sablock_test_host_chunk(const sablock_params_t* p, int n_layers, int n_seqs,
 
 static int score_kernels(const Plan& pl) { return !pl.use_tc ? (pl.use_x3 ? 1 : 0) : pl.use_pair ? 3 : pl.use_flow ? 2 : 4; }
 
-// n / d as the paged kernels compute it, and the runs that an append has at most (host only).
+// n / d as the paged kernels compute it, the runs that an append has at most, and what an append's output is checked with (host only).
+int sablock_test_meets_rows(size_t out, size_t n_out, size_t at, size_t row, size_t step, size_t n) { return meets_rows(out, n_out, at, row, step, n); }
 int sablock_test_fast_div(int n, int d) { return fast_div((uint32_t)d).div(n); }
 long long sablock_test_append_runs(long long n_tokens, int n_seqs, int run_rows, int one_each)
 {
@@ -1683,10 +1691,13 @@ sablock_status_t sablock_paged_append(const sablock_params_t* p, const sablock_p
     if ((a.k_tok * es) % 16 || (a.v_tok * es) % 16 || (a.q_tok * es) % 16 || !aligned16(k) || !aligned16(v) || !aligned16(q) || !aligned16(q_out))
         return SABLOCK_ERR_UNSUPPORTED;
     if (n_tokens == 0) return SABLOCK_OK;
-    if (q) {   // a channel's partner is read by another thread than the one that writes it
-        const uintptr_t in = reinterpret_cast<uintptr_t>(q), out = reinterpret_cast<uintptr_t>(q_out);
-        const size_t row = (size_t)a.H * a.D * es, n = (size_t)n_tokens - 1;
-        if (in < out + n * row + row && out < in + n * (size_t)a.q_tok * es + row) return SABLOCK_ERR_INVALID_ARG;
+    if (q) {   // what is read must not be written: a channel's partner and the other heads are read by other threads and CTAs
+        const uintptr_t out = reinterpret_cast<uintptr_t>(q_out);
+        const size_t n = (size_t)n_tokens, q_row = (size_t)a.H * a.D * es, kv_row = (size_t)a.Hkv * a.D * es;
+        if (meets_rows(out, n * q_row, reinterpret_cast<uintptr_t>(q), q_row, (size_t)a.q_tok * es, n) ||
+            meets_rows(out, n * q_row, reinterpret_cast<uintptr_t>(k), kv_row, (size_t)a.k_tok * es, n) ||
+            meets_rows(out, n * q_row, reinterpret_cast<uintptr_t>(v), kv_row, (size_t)a.v_tok * es, n))
+            return SABLOCK_ERR_INVALID_ARG;
     }
     a.q = q; a.k = k; a.v = v; a.q_out = q_out;
     a.cu = cu_new; a.pos = positions; a.inv_freq = inv_freq;

@@ -46,3 +46,22 @@ def test_append_with_queries_that_overlap(stride):
     freq, cu = torch.linspace(1.0, 0.001, 32, device="cuda"), torch.tensor([0, 4, 7], dtype=torch.int32, device="cuda")
     got = [B.paged_append(p, c.handle(p), x, x, q=t, positions=pos, inv_freq=freq, cu_new=cu) for t in (q, q.contiguous())]
     assert got[0].is_contiguous() and torch.equal(*got)
+
+
+def test_append_with_its_output_beside_and_over_what_it_reads():
+    """The rotated queries may go between the tokens of one projection's output, not over its parts."""
+    p, n = _params(4, 2, 64, BF16), 3
+    c = Cache([2, 1], 2, 64, 16, BF16, fill=0.0)
+    wide = c.randn(n, 8 * 64 + n * 4 * 64)                             # queries, keys and values of a token, then room for all queries
+    parts = [wide[:, 64 * a:64 * b].unflatten(1, (b - a, 64)) for a, b in ((0, 4), (4, 6), (6, 8))]
+    freq, cu = torch.linspace(1.0, 0.001, 32, device="cuda"), torch.tensor([0, 2, 3], dtype=torch.int32, device="cuda")
+    kw = dict(inv_freq=freq, cu_new=cu, positions=torch.arange(n, dtype=torch.int32, device="cuda") * 5)
+    ref = B.paged_append(p, c.handle(p), parts[1], parts[2], q=parts[0], **kw)
+    before = wide[:, :8 * 64].clone()
+    for row in range(n):
+        gap = wide[row, 8 * 64:].view(n, 4, 64)
+        assert torch.equal(B.paged_append(p, c.handle(p), parts[1], parts[2], q=parts[0], q_out=gap, **kw), ref)
+    for start in (0, 5 * 64, 7 * 64, 8 * 64 + 64):                     # the last one begins in the room and ends in the next token
+        with pytest.raises(B.SablockError):
+            B.paged_append(p, c.handle(p), parts[1], parts[2], q=parts[0], q_out=wide.flatten()[start:start + n * 256].view(n, 4, 64), **kw)
+    assert torch.equal(wide[:, :8 * 64], before)

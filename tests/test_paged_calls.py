@@ -1,12 +1,14 @@
 """What the binding's calls over a paged cache do with a call that they refuse, with blocks and tensors that change, with nothing to do:
 on the host (no GPU), the entry points themselves replaced where a good call would enqueue work."""
 import ctypes as C
+import random
 
 import pytest
 import torch
 
 from paper_2510_22556_b200 import binding as B
 from paper_2510_22556_b200 import build as build_lib
+from paper_2510_22556_b200.build import build_test_hooks
 
 
 @pytest.fixture(scope="module", autouse=True)
@@ -183,3 +185,36 @@ def test_appending_no_tokens(monkeypatch, through_module):
         B.paged_append(p, g, x, x)
     with pytest.raises(B.SablockError):
         B.paged_append(p, g, x, x, cu_new=cu, inv_freq=torch.ones(9))
+
+
+FAKE = 1 << 30                                     # never dereferenced
+
+
+@pytest.mark.parametrize("array", ["q", "k", "v"])
+@pytest.mark.parametrize("stride", [0, 768])       # contiguous; the parts of one projection's output
+def test_rotated_queries_over_an_array_that_is_read(array, stride):
+    """Another CTA may not have read the tokens that such a write falls on."""
+    p, n, heads = _params(8, 2, 64, torch.bfloat16), 5, 8 if array == "q" else 2
+    g = B.Pages()
+    g.k, g.v, g.table, g.seq_lens = FAKE << 1, FAKE << 2, FAKE << 3, FAKE << 4
+    g.n_seqs, g.n_pages, g.page_size, g.max_pages = n, 100, 64, 20
+    at = dict(q=FAKE + (1 << 20), k=FAKE + (2 << 20), v=FAKE + (3 << 20))
+    last = at[array] + ((n - 1) * (stride or heads * 64) + heads * 64) * 2         # behind the last token
+    for q_out in (at[array], last - 16, at[array] - n * 8 * 64 * 2 + 16):
+        code = B.lib().paged_append(C.addressof(p), C.addressof(g), n, None, at["k"], stride, at["v"], stride, at["q"], stride, q_out, None, None, 0, 0, None)
+        assert code == 1
+
+
+def test_what_meets_the_rows_of_an_array():
+    """Bytes against rows that lie apart, side by side or over one another, byte by byte."""
+    hooks = C.CDLL(build_test_hooks())
+    hooks.sablock_test_meets_rows.argtypes = [C.c_size_t] * 6
+    r = random.Random(3)
+    seen = [0, 0]
+    for _ in range(4000):
+        out, n_out, at, row, step, n = r.randint(50, 150), r.randint(1, 40), r.randint(50, 150), r.randint(1, 20), r.randint(1, 40), r.randint(1, 6)
+        rows = {at + i * step + b for i in range(n) for b in range(row)}
+        want = not rows.isdisjoint(range(out, out + n_out))
+        seen[want] += 1
+        assert bool(hooks.sablock_test_meets_rows(out, n_out, at, row, step, n)) == want
+    assert min(seen) > 800
