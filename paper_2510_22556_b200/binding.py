@@ -508,6 +508,14 @@ def _pages_stream(p: Params, pages: Pages) -> int:
     return torch._C._cuda_getCurrentRawStream(dev)
 
 
+def _check_choice(pages: Pages, n_selected: int, n_first: int, n_last: int, where: str) -> None:
+    """Refuses what the entry point would, before a list of that size is allocated and the numbers are cut to 32 bits."""
+    if n_selected < 1 or n_first < 0 or n_last < 0 or n_first + n_last > n_selected:
+        raise SablockError(1, where)
+    if n_selected * pages.page_size > 1 << 30:                                     # (rows that a sequence can have)
+        raise SablockError(2, where)
+
+
 def _like(p: Params, pages: Pages, n_selected: int):
     """What the scratch (None where a call needs none) and the page list of such a call look like; kept with the handle, so the block
     has been found to be the cache's (_pages_stream) before."""
@@ -586,6 +594,7 @@ def paged_attention(p: Params, pages: Pages, q: torch.Tensor, selected: Optional
 def page_select(p: Params, pages: Pages, q: torch.Tensor, n_selected: int, n_first: int = 1, n_last: int = 1) -> torch.Tensor:
     """The pages whose bounds promise the largest logits, per KV head: int32 [n_seqs, Hkv, n_selected], ascending, then -1."""
     q_at = _contiguous("q", q, pages._dtype, pages._device, pages._q_shape)
+    _check_choice(pages, n_selected, n_first, n_last, "sablock_page_select")
     stream = _pages_stream(p, pages)
     selected = torch.empty_like(_like(p, pages, n_selected)[1])
     _check(lib().page_select(C.addressof(p), C.addressof(pages), q_at, n_selected, n_first, n_last, _ptr(selected), stream),
@@ -597,6 +606,7 @@ def paged_sparse_attention(p: Params, pages: Pages, q: torch.Tensor, n_selected:
                            ws: Optional[torch.Tensor] = None, want_lse: bool = False):
     """page_select and paged_attention over what it selects.  Returns (out, selected), and lse behind them."""
     q_at = _contiguous("q", q, pages._dtype, pages._device, pages._q_shape)
+    _check_choice(pages, n_selected, n_first, n_last, "sablock_paged_sparse_attention")
     stream = _pages_stream(p, pages)
     out = torch.empty_like(q, dtype=torch.float32)
     lse = torch.empty_like(pages._lse_like) if want_lse else None

@@ -1744,7 +1744,7 @@ sablock_status_t sablock_paged_append(const sablock_params_t* p, const sablock_p
 size_t sablock_paged_workspace_bytes(const sablock_params_t* p, const sablock_pages_t* pages, int n_selected)
 {
     Paged pg;
-    if (paged_args(p, pages, &pg) != SABLOCK_OK) return 0;
+    if (paged_args(p, pages, &pg) != SABLOCK_OK || n_selected < -1 || (long long)n_selected * pg.page_size > kPgMaxRows) return 0;
     return n_selected >= 0 && paged_cluster(p, pg, n_selected) ? 16 : paged_plan(p).bytes;
 }
 

@@ -218,3 +218,24 @@ def test_what_meets_the_rows_of_an_array():
         seen[want] += 1
         assert bool(hooks.sablock_test_meets_rows(out, n_out, at, row, step, n)) == want
     assert min(seen) > 800
+
+
+@pytest.mark.parametrize("n,kw,code", [
+    (0, {}, 1), (-1, {}, 1), (-5, {}, 1), (4, dict(n_first=-1), 1), (4, dict(n_first=3, n_last=2), 1), (4, dict(n_first=1 << 32), 1), (4, dict(n_last=(1 << 32) + 1), 1),
+    (1 << 29, {}, 2), ((1 << 32) + 4, {}, 2), (1 << 45, {}, 2)])
+def test_a_choice_that_cannot_be_is_refused_before_its_list_is_allocated(entry, n, kw, code):
+    """Pages of four rows: 2^28 pages are as many rows as a sequence can have.  Numbers past 32 bits are not cut to their low ones."""
+    p = _params()
+    g, q = _cache(p), torch.zeros(2, 8, 16)
+    for call in (lambda: B.page_select(p, g, q, n, **kw), lambda: B.paged_sparse_attention(p, g, q, n, **kw)):
+        with pytest.raises(B.SablockError) as e:
+            call()
+        assert e.value.code == code
+    assert not entry.calls and not g._like
+
+
+def test_scratch_of_a_choice_that_cannot_be():
+    p = _params()
+    g = _cache(p)
+    need = [int(B.lib().sablock_paged_workspace_bytes(C.addressof(p), C.addressof(g), n)) for n in (-1, 0, 1 << 28, (1 << 28) + 1, -2)]
+    assert min(need[:3]) > 0 and need[3:] == [0, 0]
