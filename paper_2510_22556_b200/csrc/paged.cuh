@@ -56,10 +56,6 @@ template <> struct PgVec<float> {
     {
         x[0] = __uint_as_float(u.x); x[1] = __uint_as_float(u.y); x[2] = __uint_as_float(u.z); x[3] = __uint_as_float(u.w);
     }
-    __device__ static uint4 pack(const float (&x)[4])
-    {
-        return make_uint4(__float_as_uint(x[0]), __float_as_uint(x[1]), __float_as_uint(x[2]), __float_as_uint(x[3]));
-    }
     __device__ static float round(float x) { return x; }
 };
 template <> struct PgVec<__nv_bfloat16> {
@@ -72,16 +68,6 @@ template <> struct PgVec<__nv_bfloat16> {
             x[2 * i] = __uint_as_float(w[i] << 16);
             x[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
         }
-    }
-    __device__ static uint4 pack(const float (&x)[8])
-    {
-        uint32_t w[4];
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const __nv_bfloat162 t = __floats2bfloat162_rn(x[2 * i], x[2 * i + 1]);
-            w[i] = *reinterpret_cast<const uint32_t*>(&t);
-        }
-        return make_uint4(w[0], w[1], w[2], w[3]);
     }
     __device__ static __nv_bfloat16 round(float x) { return __float2bfloat16_rn(x); }
 };
