@@ -291,7 +291,7 @@ sablock_status_t sablock_decode_attention(const sablock_params_t *p, int n_prob,
  *
  * head_dim * element size must be a multiple of 16 bytes and head_dim at most 256; pools, strides, queries, tokens and
  * workspace on 16-byte boundaries (SABLOCK_ERR_UNSUPPORTED otherwise; a misplaced workspace is SABLOCK_ERR_INVALID_ARG).  Any
- * number of query heads per KV head, any page size.  Up to 4096 sequences of up to 2^30 rows.
+ * number of query heads per KV head (n_q_heads at most 4096), any page size.  Up to 4096 sequences of up to 2^30 rows.
  * Device data that says what cannot be stays inside the buffers: lengths are taken as at least 0 and at most
  * max_pages * page_size, and a page number outside [0, n_pages) is not followed (append drops the row, attention treats it as
  * absent).  Two rows of one append that fall on the same place (a page that is in two tables) leave either's values.  The device arrays
@@ -328,7 +328,8 @@ size_t sablock_pages_sizeof(void);   /* sizeof(sablock_pages_t) as the library w
  *  rotated already, go into pages): the first rotary_dim channels of a head are turned in pairs (i, i + rotary_dim / 2), or
  *  (2 i, 2 i + 1) with interleaved, by the angle position * inv_freq[i].  positions dev int32[n_tokens] or NULL (the
  *  row number).  After a compression a token's position is not its row: pass positions.
- *  The angle is formed in 64 bits modulo a turn, the rotation computed in fp32 and rounded once to dtype.
+ *  The angle is formed in 64 bits modulo a turn (for inv_freq <= 1 off by less than 2^-31 of a turn up to position 2^22, by 2^-24 at the last), the
+ *  rotation computed in fp32 and rounded once to dtype.
  *  With bounds: those of the pages that rows fall into are brought up to date; the first row of a page starts them anew.  Bounds hold no number
  *  where a key does not. */
 sablock_status_t sablock_paged_append(const sablock_params_t *p, const sablock_pages_t *pages, int n_tokens,
@@ -340,9 +341,9 @@ sablock_status_t sablock_paged_append(const sablock_params_t *p, const sablock_p
 /* The attention of one new query token per sequence over the rows of its pages (as sablock_decode_attention):
  *  q dev [n_seqs, H, D] contiguous; out dev f32 [n_seqs, H, D]; lse dev f32 [n_seqs, H] or NULL.
  *  selected NULL (n_selected 0): every row.  Otherwise dev int32 [n_seqs, Hkv, n_selected]: for each KV head the pages of the sequence
- *  (0 for its first) whose rows count; of a sequence with fewer pages than n_selected as many entries are
+ *  (0 for its first) whose rows count (n_selected * page_size at most 2^30); of a sequence with fewer pages than n_selected as many entries are
  *  read as it has pages; entries outside the sequence (-1) count nothing, an entry that stands twice counts twice.
- *  A sequence without rows gets zeros and -inf.  Scratch from ws; nothing in it has to be set.  Accumulation is fp32 in an order that
+ *  A sequence without rows gets zeros and -inf.  What a call writes, scratch included, shares no byte with what it reads.  Scratch from ws; nothing in it has to be set.  Accumulation is fp32 in an order that
  *  the lengths of the call fix.
  * sablock_paged_workspace_bytes: the bytes of ws for a call over all rows (n_selected 0), for sablock_paged_sparse_attention with
  *  n_selected pages, and for any call (n_selected -1, also the one for a given list); 0 on invalid arguments, 16 where the call

@@ -532,7 +532,8 @@ def paged_append(p: Params, pages: Pages, k: torch.Tensor, v: torch.Tensor, q: O
                  positions: Optional[torch.Tensor] = None, inv_freq: Optional[torch.Tensor] = None, interleaved: bool = False,
                  cu_new: Optional[torch.Tensor] = None, q_out: Optional[torch.Tensor] = None) -> Optional[torch.Tensor]:
     """New tokens k, v [n, Hkv, D] become the last rows of their sequences (cu_new int32 [n_seqs + 1]: whose they are; None: one
-    each), keys and queries q [n, H, D] rotated by positions * inv_freq on the way.  Returns the rotated queries."""
+    each), keys and queries q [n, H, D] rotated by positions * inv_freq on the way.  Returns the rotated queries; the rows of tokens that
+    have no place (behind the last sequence, of an empty one, past the table) are not written, in a result made here as in q_out."""
     l, fast = lib(), pages._fast
     if l.append_step is not None and fast is not None:
         done = l.append_step(C.addressof(p), C.addressof(pages), fast, k, v, q, q_out, positions, inv_freq, interleaved, cu_new, _pages_stream(p, pages))
@@ -569,7 +570,7 @@ def paged_append(p: Params, pages: Pages, k: torch.Tensor, v: torch.Tensor, q: O
 def paged_attention(p: Params, pages: Pages, q: torch.Tensor, selected: Optional[torch.Tensor] = None,
                     ws: Optional[torch.Tensor] = None, want_lse: bool = False):
     """Attention of one new token per sequence, q [n_seqs, H, D], over the rows of its pages, or over the pages selected int32
-    [n_seqs, Hkv, n].  Returns out f32 [n_seqs, H, D] (and lse [n_seqs, H])."""
+    [n_seqs, Hkv, n], n > 0.  Returns out f32 [n_seqs, H, D] (and lse [n_seqs, H])."""
     q_at = _contiguous("q", q, pages._dtype, pages._device, pages._q_shape)
     sel_at, n = None, 0
     if selected is not None:

@@ -91,7 +91,9 @@ __device__ __forceinline__ float max_nan(float a, float b)
 // come in pairs (d, d + rd / 2), or (2 i, 2 i + 1) interleaved, and a pair is turned by the angle position * inv_freq[i]:
 //   x' = x cos - y sin,  y' = y cos + x sin,
 // in fp32, rounded once to the cache's type.  The angle needs more than 32 bits (at position 10^6 an fp32 angle is off by 0.03): as turns,
-// position * inv_freq / 2 pi, it is formed modulo one in 64-bit fixed point, which at the last position is off by 2^-33.
+// position * inv_freq / 2 pi, it is formed modulo one in 64-bit fixed point from the turn per position, a product in double that is off by
+// at most 2^-52.3 of itself.  For inv_freq <= 1 (0.16 turns) that is less than the 2^-32 of a turn that the angle is cut to up to position 2^22,
+// and 2^-24 at the last one, 2^31 - 1; rounding it to the fp32 argument of the sine adds up to 2^-26.
 //
 // A CTA has one run of rows of one sequence, at most kApRun of them and aligned, and its KV heads with their query heads.  A warp takes a
 // token at a time (where a run has fewer tokens than the CTA warps, several share one): it makes the token's cosines and sines once
@@ -102,10 +104,13 @@ __device__ __forceinline__ float max_nan(float a, float b)
 //
 // Bounds of a page have one writer, a CTA that has all its new rows: the one that writes them, where a page has no more than
 // kApBoundsRun rows or a sequence has one new token; a second launch elsewhere, which reads the keys again (in L2).  Pages of 64 rows
-// in the first launch leave 165 CTAs for 10000 tokens: 69 us, two launches 67; pages of 32 rows 30 us, two launches 33.
+// in the first launch leave 214 CTAs for the 13419 tokens of five prompts: 69 us, two launches 67; 16384 rows into pages of 32 rows, 512
+// CTAs: 30 us, two launches 33.  (Both points are of calls that fill the device; the rule goes by the page's rows alone.)
 //
-// Bound by memory: every row is read and written once.  10106 tokens of five prompts, 32 + 8 + 8 heads of 128, 332 MB in 68 us = 4.9
-// TB/s (75 % of a copy's rate; without bounds 5.6 TB/s); 16384 retained rows, 138 MB in 30 us.  One token is a chain of latencies, 4 us.
+// Long calls are bound by memory, every row being read and written once: 13419 tokens of five prompts, 32 + 8 + 8 heads of 128, 332 MB in
+// 69 us = 4.8 TB/s (74 % of a copy's rate; without bounds 5.6 TB/s).  With bounds in the same launch a thread has 127 registers, two CTAs an SM,
+// rotation or not: 16384 retained rows, 138 MB in 30.6 us = 4.5 TB/s, are 512 CTAs on 296 places, 1.7 turns of them, each with its look-ups ahead of its
+// rows.  Without bounds it has the 80 that three CTAs an SM leave, and 36 bytes are spilled.  One token is a chain of latencies, 4 us.
 constexpr int kApThreads = 256;
 constexpr int kApRun = 16;
 constexpr int kApBoundsRun = 32;                            // rows of a page whose bounds the same CTA makes

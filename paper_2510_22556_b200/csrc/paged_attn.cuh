@@ -12,9 +12,9 @@
 // in one share are written out; of the others every share leaves (accumulator, maximum, sum) in scratch, at most one at its
 // start and one at its end, and paged_merge_kernel, one block per share and head, adds up the pairs that begin in its share.
 //
-// Bound by memory where there is work for the device: one sequence of 128K rows, 8 KV heads of 128, 537 MB in 84 us = 6.4 TB/s (98 % of a
-// copy's rate); 16 sequences of 4K to 16K rows 578 MB in 95 us; 64 sequences of 1K to 1.5K rows, 331 MB in 63 us, of which 8 are
-// the two launches, the sum over the lengths and the first look-ups.
+// Bound by memory where there is work for the device: one sequence of 128K rows, 8 KV heads of 128, 537 MB in 87 to 94 us a call, from one B200 to
+// another, = 5.7 to 6.2 TB/s (88 to 95 % of a copy's rate; 84 in a graph of calls); 16 sequences of 4K to 16K rows 578 MB in 95 to 103 us; 64
+// sequences of 1K to 1.5K rows, 331 MB in 63 to 67 us, of which 8 are the two launches, the sum over the lengths and the first look-ups.
 //
 // A row is found through the table (and the list of chosen pages): the lanes of a warp look up the sixteen rows of a
 // chunk one turn before its copies go out (two turns before for the list), so the look-ups are never waited for.  Rows that do not
@@ -218,6 +218,8 @@ __device__ __forceinline__ void pg_emit4(const PagedAttnArgs& a, const PgSegment
 // the weights of a set take two instructions, half of the leading pieces in rows 0-7 of either (zeros there would make no numbers
 // of infinite values), the middle pieces in rows 8-15 of one and the last ones of the other.
 // head_dim is padded to DP with zeros that are not read from memory.
+// All 255 registers are used.  Two sets at 128 channels (9 to 16 heads) spill 176 bytes of a thread and read 276 back, one set at 256 channels 112 and
+// 104: with four products of weights and values for a pair of sets, that is why the warps' own work and not memory bounds these two.
 constexpr int kPaThreads = 128;
 constexpr int kPaWarps = kPaThreads / 32;
 constexpr int kPaStages = 3;
